@@ -236,6 +236,118 @@ int qsgd_pipeline_step(qsgd_pipeline *pl, const qsgd_params *p, uint64_t chunk_e
                        void *const *msg_dev, size_t msg_capacity, void *enc_workspace_dev,
                        void *dec_workspace_dev, size_t workspace_bytes, void *hip_stream);
 
+/* ---- A layer in 8 bits: what makes the gradient that qsgd_encode takes.  The quantizer of
+ * Sec. 3.1 with s = 127 levels and the largest magnitude as scale (Sec. 4), a bucket being a
+ * row or a column of a matrix; the product of two such matrices in integers; a linear layer
+ * made of them with its gradients; and dropout from the same counter-based generator.
+ * All draws are reproducible from their key and position, no mask or generator state is stored.
+ */
+
+/* Element types of a matrix. */
+#define QSGD_TYPE_F32  0u
+#define QSGD_TYPE_BF16 1u
+#define QSGD_TYPE_F16  2u
+#define QSGD_TYPE_I8   3u
+
+#define QSGD_ROUND_NEAREST    0u /* to the nearest level, ties to the even one              */
+#define QSGD_ROUND_STOCHASTIC 1u /* to one of the two levels around the value, unbiased      */
+
+/* A matrix in device memory: element (r, c) is at data_dev[r * ld + c].  rows, cols < 2^31,
+ * rows * ld < 2^46.  ld >= cols; the data are aligned to their element's size (rows that are 16
+ * bytes apart modulo 16 and start at a multiple of 16 bytes are faster).  Matrices of QSGD_TYPE_I8
+ * are aligned to 16 bytes, ld is a multiple of 16, and the bytes of a row up to the next
+ * multiple of 16 are readable; what stands there changes no result and is not written.
+ * data_dev may be NULL where rows or cols is 0. */
+typedef struct qsgd_matrix {
+  void *data_dev;
+  uint64_t rows, cols, ld;
+  uint32_t type;
+  uint32_t reserved; /* must be 0 */
+} qsgd_matrix;
+
+/* The draws of a matrix: element (r, c) has the half-word c % 8 (two to a word, the low one
+ * first) of the Philox-4x32-10 block with counter (c / 8, row_base + r, stream_id, iteration)
+ * and key seed.  A slice of rows passes the number of its first row as row_base
+ * (row_base + rows <= 2^32).  iteration_dev, a word in device memory or NULL, is added to
+ * iteration when the kernels run, so that a captured graph draws anew at each replay. */
+typedef struct qsgd_draws {
+  uint64_t seed;
+  uint32_t stream_id;
+  uint32_t iteration;
+  uint32_t row_base;
+  uint32_t reserved; /* must be 0 */
+  const uint32_t *iteration_dev;
+} qsgd_draws;
+
+/* Dropout:  y = residual + keep * x * 65536 / (65536 - D),  D = rint(65536 p), 0 <= p <= 1;
+ * keep is whether the element's draw h >= D, so an element is dropped with probability D / 65536
+ * exactly and E y = residual + x (p = 1 or nearest to it drops everything).  A dropped element
+ * contributes +0 whatever its value.  Computed in fp32, rounded once to y's type.  x, residual
+ * (NULL: none) and y have one shape and one type of F32, BF16, F16; y may be x or residual
+ * itself (same data_dev and ld), otherwise it must not overlap them. */
+int qsgd_dropout(const qsgd_draws *draws, float p, const qsgd_matrix *x,
+                 const qsgd_matrix *residual, const qsgd_matrix *y, void *hip_stream);
+
+/* Its gradient with the same draws and p:  dx = keep * dy * 65536 / (65536 - D).  (The gradient
+ * of the residual is dy.)  dx may be dy itself. */
+int qsgd_dropout_backward(const qsgd_draws *draws, float p, const qsgd_matrix *dy,
+                          const qsgd_matrix *dx, void *hip_stream);
+
+/* Quantizer by rows, by columns, or both:  with m the largest magnitude of the row (column),
+ *   scale = m / 127,  t = |x| fl(127 / m) in fp32,  level = sgn(x) rint(t)                 (nearest)
+ *                                                   level = sgn(x) (floor(t) + [u < t - floor(t)])  (stochastic)
+ * with u = (h + 1/2) / 65536, h the element's draw (the same one in both forms); at most 127.
+ * A row with m < 2^-119 counts as zero (scale 0, levels 0); one that holds an infinity or a NaN
+ * gets scale NaN and levels 0, so that whatever is computed from it is NaN.
+ *   x           F32, BF16 or F16
+ *   rows        out: levels, I8, the shape of x (or NULL); row_scale_dev: x->rows floats
+ *   columns     out: levels TRANSPOSED, I8, x->cols rows of x->rows values (or NULL);
+ *               column_scale_dev: x->cols floats
+ *   workspace   device, 16-byte aligned, >= qsgd_quantize_workspace_bytes(x->rows, x->cols);
+ *               not used (NULL, 0) without columns
+ *   draws       may be NULL for QSGD_ROUND_NEAREST */
+size_t qsgd_quantize_workspace_bytes(uint64_t rows, uint64_t cols);
+int qsgd_quantize(const qsgd_draws *draws, uint32_t rounding, const qsgd_matrix *x,
+                  const qsgd_matrix *rows, float *row_scale_dev, const qsgd_matrix *columns,
+                  float *column_scale_dev, void *workspace_dev, size_t workspace_bytes,
+                  void *hip_stream);
+
+/* Product of 8-bit matrices:  y[m][n] = (sum_k a[m][k] b[n][k]) a_scale[m] b_scale[n] + bias[n].
+ * The sum is exact (32-bit integers, joined in 64 bits where they could pass); the factors are
+ * applied in fp32, the smaller scale first, and the result is rounded once to y's type.
+ *   a  M x K, I8, with M scales;  b  N x K, I8, with N scales;  bias_dev  N floats or NULL
+ *   y  M x N, F32, BF16 or F16; must not overlap the operands
+ *   workspace  device, 16-byte aligned, >= qsgd_int_matmul_workspace_bytes(M, N, K), calls sharing
+ *              it must not overlap; NULL where that is 0
+ * QSGD_ERR_UNSUPPORTED: rows of the operands 2^23 bytes apart or more. */
+size_t qsgd_int_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K);
+int qsgd_int_matmul(const qsgd_matrix *a, const float *a_scale_dev, const qsgd_matrix *b,
+                    const float *b_scale_dev, const float *bias_dev, const qsgd_matrix *y,
+                    void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* Linear layer, forward:  y = Q(x) W^T + bias, Q the quantizer by rows (tokens), W the weights as
+ * qsgd_quantize left them by rows (outputs x inputs, a scale per output).  x, y: one type of
+ * F32, BF16, F16.  The result is that of qsgd_quantize and qsgd_int_matmul. */
+size_t qsgd_linear_forward_workspace_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs);
+int qsgd_linear_forward(const qsgd_draws *draws, uint32_t rounding, const qsgd_matrix *x,
+                        const qsgd_matrix *w, const float *w_scale_dev, const float *bias_dev,
+                        const qsgd_matrix *y, void *workspace_dev, size_t workspace_bytes,
+                        void *hip_stream);
+
+/* Its gradients, from the unquantized x (tokens x inputs), w (outputs x inputs) and dy (tokens x
+ * outputs), one type of F32, BF16, F16:
+ *   dx = Q_row(dy) Q_col(w)      that type         (or NULL)
+ *   dw = Q_col(dy)^T Q_col(x)    F32: the gradient that qsgd_encode takes   (or NULL)
+ *   db = sum over the tokens of dy, in fp32        (or NULL)
+ * dy draws with stream_id, w with stream_id + 1 (its rows counted from 0), x with
+ * stream_id + 2.  With stochastic rounding the factors are independent, so that E dx = dy w and
+ * E dw = dy^T x: unbiased estimates of the gradient, as Algorithm 1 asks of g. */
+size_t qsgd_linear_backward_workspace_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs);
+int qsgd_linear_backward(const qsgd_draws *draws, uint32_t rounding, const qsgd_matrix *x,
+                         const qsgd_matrix *w, const qsgd_matrix *dy, const qsgd_matrix *dx,
+                         const qsgd_matrix *dw, float *db_dev, void *workspace_dev,
+                         size_t workspace_bytes, void *hip_stream);
+
 /* Reads a message header from a HOST copy of (at least) its first 64 bytes.
  * Fills *out (seed is not stored: 0) and *total_bytes (either may be NULL).
  * Returns 0, QSGD_ERR_CORRUPT (not a header), or the status the encoder left

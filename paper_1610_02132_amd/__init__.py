@@ -14,4 +14,7 @@ from .binding import (  # noqa: F401
     qsgd_layout_max_encoded_bytes, qsgd_layout_workspace_bytes, qsgd_sgd_step_layout,
     Pipeline, qsgd_encode_slice, qsgd_pipeline_step, qsgd_copy_probe_words,
     qsgd_encode_workspace_bytes, qsgd_encode_static, qsgd_static_scratch_bytes,
+    ROUND_NEAREST, ROUND_STOCHASTIC, Draws, qsgd_dropout, qsgd_dropout_backward, qsgd_quantize,
+    qsgd_quantize_workspace_bytes, qsgd_int_matmul, qsgd_int_matmul_workspace_bytes, qsgd_linear_forward,
+    qsgd_linear_forward_workspace_bytes, qsgd_linear_backward, qsgd_linear_backward_workspace_bytes,
 )

@@ -292,30 +292,6 @@ std::vector<TimedLaunch> g_launches;
 std::vector<EventPair> g_spare;
 constexpr size_t kSpareEvents = 1024;
 
-struct ScopedTiming {
-  hipStream_t st; bool on; TimedLaunch t;
-  ScopedTiming(const char* name, hipStream_t s) : st(s), on(false) {
-    std::lock_guard<std::mutex> lk(g_timing_mu);
-    if (!g_timing_on) return;
-    if (!g_spare.empty()) {
-      t.start = g_spare.back().start; t.stop = g_spare.back().stop;
-      g_spare.pop_back();
-    } else {
-      if (hipEventCreate(&t.start) != hipSuccess) return;
-      if (hipEventCreate(&t.stop) != hipSuccess) { (void)hipEventDestroy(t.start); return; }
-    }
-    t.name = name;
-    on = hipEventRecord(t.start, st) == hipSuccess;
-    if (!on) g_spare.push_back({t.start, t.stop});
-  }
-  ~ScopedTiming() {
-    if (!on) return;
-    (void)hipEventRecord(t.stop, st);
-    std::lock_guard<std::mutex> lk(g_timing_mu);
-    g_launches.push_back(t);
-  }
-};
-
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Geometry of a tensor-aware message: the layout says how many buckets there are.
@@ -657,6 +633,31 @@ __global__ __launch_bounds__(256) void k_copy_probe_words(uint32_t* __restrict__
        i += (uint64_t)gridDim.x * 256)
     dst[i] = src[i];
 }
+
+namespace qsgd {
+
+ScopedTiming::ScopedTiming(const char* what, hipStream_t s) : st(s), name(what) {
+  std::lock_guard<std::mutex> lk(g_timing_mu);
+  if (!g_timing_on) return;
+  if (!g_spare.empty()) {
+    start = g_spare.back().start; stop = g_spare.back().stop;
+    g_spare.pop_back();
+  } else {
+    if (hipEventCreate(&start) != hipSuccess) return;
+    if (hipEventCreate(&stop) != hipSuccess) { (void)hipEventDestroy(start); return; }
+  }
+  on = hipEventRecord(start, st) == hipSuccess;
+  if (!on) g_spare.push_back({start, stop});
+}
+
+ScopedTiming::~ScopedTiming() {
+  if (!on) return;
+  (void)hipEventRecord(stop, st);
+  std::lock_guard<std::mutex> lk(g_timing_mu);
+  g_launches.push_back({name, start, stop});
+}
+
+}  // namespace qsgd
 
 extern "C" {
 

@@ -258,6 +258,16 @@ struct GenArgs {
   uint64_t fixed_payload_words;
 };
 
+// Brackets the launches in its scope by a pair of events while qsgd_timing_enable is on.
+struct ScopedTiming {
+  hipStream_t st;
+  const char* name;   // a literal
+  bool on = false;
+  hipEvent_t start = nullptr, stop = nullptr;
+  ScopedTiming(const char* what, hipStream_t s);
+  ~ScopedTiming();
+};
+
 // Host-side checks of an encode / a decode call that only depend on the parameters and the
 // buffer sizes (what the entry points test before they queue anything): 0 or a QSGD_ERR_*.
 int validate_encode(const qsgd_params* p, uint64_t index_base, size_t msg_capacity,

@@ -1,0 +1,369 @@
+// C ABI of the operators of a layer in 8 bits (see include/qsgd.h): checks of arguments, workspace
+// layout, kernel launches.  Everything is checked before anything is queued.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "qsgd.h"
+#include "qsgd_kernels.hpp"
+#include "qsgd_layer.hpp"
+
+namespace {
+
+using namespace qsgd;
+
+bool aligned(const void* p, uint64_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+uint64_t size_of(uint32_t type) { return type == QSGD_TYPE_F32 ? 4 : type == QSGD_TYPE_I8 ? 1 : 2; }
+
+uint64_t padded(uint64_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// A matrix as the header describes it: of levels (I8) or of values.
+bool sound(const qsgd_matrix* m, bool levels) {
+  if (!m || m->reserved || m->rows >= 1ull << 31 || m->cols >= 1ull << 31 || m->ld < m->cols || m->ld >= 1ull << 46 ||
+      (levels ? m->type != QSGD_TYPE_I8 : m->type > QSGD_TYPE_F16))
+    return false;
+  if (m->rows && m->ld >= (1ull << 46) / m->rows) return false;
+  if (m->rows == 0 || m->cols == 0) return true;
+  return m->data_dev && aligned(m->data_dev, levels ? 16 : size_of(m->type)) && !(levels && m->ld % 16);
+}
+
+bool shaped(const qsgd_matrix* m, uint64_t rows, uint64_t cols) { return m->rows == rows && m->cols == cols; }
+
+// Every row starts at a multiple of 16 bytes.
+bool wide(const qsgd_matrix* m) {
+  return aligned(m->data_dev, 16) && (m->rows <= 1 || m->ld * size_of(m->type) % 16 == 0);
+}
+
+// Bytes [first, second) that a matrix covers.
+struct Span { uintptr_t from, to; };
+Span span(const qsgd_matrix* m) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(m->data_dev);
+  if (!m->rows || !m->cols) return {p, p};
+  return {p, p + ((m->rows - 1) * m->ld + m->cols) * size_of(m->type)};
+}
+bool overlap(const qsgd_matrix* x, const qsgd_matrix* y) {
+  const Span a = span(x), b = span(y);
+  return a.from < b.to && b.from < a.to;
+}
+bool same_place(const qsgd_matrix* x, const qsgd_matrix* y) {
+  return x->data_dev == y->data_dev && (x->ld == y->ld || x->rows <= 1);
+}
+
+bool floats(const float* p, uint64_t n) { return n == 0 || (p && aligned(p, 4)); }
+
+int draw_args(const qsgd_draws* d, uint64_t rows, DrawArgs& a) {
+  if (!d || d->reserved || d->row_base + rows > 1ull << 32 || !aligned(d->iteration_dev, 4)) return QSGD_ERR_INVALID_ARG;
+  a = {(uint32_t)d->seed, (uint32_t)(d->seed >> 32), d->stream_id, d->iteration, d->row_base, d->iteration_dev};
+  return QSGD_OK;
+}
+
+int status(hipError_t e) { return e == hipSuccess ? QSGD_OK : QSGD_ERR_HIP; }
+
+int dropout(const qsgd_draws* draws, float p, const qsgd_matrix* x, const qsgd_matrix* residual, const qsgd_matrix* y,
+            const char* name, hipStream_t st) {
+  if (!(p >= 0.0f && p <= 1.0f) || !sound(x, false) || !sound(y, false) || (residual && !sound(residual, false)))
+    return QSGD_ERR_INVALID_ARG;
+  if (!shaped(y, x->rows, x->cols) || y->type != x->type) return QSGD_ERR_INVALID_ARG;
+  if (residual && (!shaped(residual, x->rows, x->cols) || residual->type != x->type)) return QSGD_ERR_INVALID_ARG;
+  if (overlap(x, y) && !same_place(x, y)) return QSGD_ERR_INVALID_ARG;
+  if (residual && overlap(residual, y) && !same_place(residual, y)) return QSGD_ERR_INVALID_ARG;
+  DropoutArgs a = {};
+  if (int rc = draw_args(draws, x->rows, a.draws)) return rc;
+  if (x->rows * ((x->cols + 7) / 8) > (1ull << 40)) return QSGD_ERR_UNSUPPORTED;
+  if (x->rows == 0 || x->cols == 0) return QSGD_OK;
+  a.x = x->data_dev; a.x_ld = x->ld;
+  a.y = y->data_dev; a.y_ld = y->ld;
+  if (residual) { a.residual = residual->data_dev; a.residual_ld = residual->ld; }
+  a.rows = (uint32_t)x->rows; a.cols = (uint32_t)x->cols;
+  a.drop = (uint32_t)std::nearbyint(65536.0 * (double)p);
+  a.scale = a.drop == 65536 ? 0.0f : 65536.0f / (float)(65536 - a.drop);
+  a.wide = wide(x) && wide(y) && (!residual || wide(residual));
+  ScopedTiming tm(name, st);
+  return status(launch_dropout(a, x->type, st));
+}
+
+// ---- quantizer -------------------------------------------------------------------
+
+// Workspace of a column form.
+struct ColumnSpace {
+  uint32_t chunks, chunk_rows;
+  uint64_t max_at, sum_at, inv_at, bytes;
+};
+ColumnSpace column_space(uint64_t rows, uint64_t cols) {
+  ColumnSpace s = {};
+  plan_columns((uint32_t)rows, (uint32_t)cols, s.chunks, s.chunk_rows);
+  const uint64_t each = padded(4 * cols * s.chunks);
+  s.max_at = 0;
+  s.sum_at = each;
+  s.inv_at = 2 * each;
+  s.bytes = 2 * each + padded(4 * cols);
+  return s;
+}
+
+void fill(QuantizeArgs& q, const qsgd_matrix* x, const DrawArgs& draws, bool stochastic) {
+  q.x = x->data_dev; q.ld = x->ld;
+  q.rows = (uint32_t)x->rows; q.cols = (uint32_t)x->cols;
+  q.wide = wide(x);
+  q.stochastic = stochastic;
+  q.draws = draws;
+}
+// scale: or null, where only the sums are wanted (levels without rows have no address either)
+void fill_columns(QuantizeArgs& q, const ColumnSpace& s, uint8_t* ws, int8_t* levels, uint64_t ld, float* scale, float* sum) {
+  q.q_cols = levels; q.q_cols_ld = ld; q.col_scale = scale;
+  q.chunks = s.chunks; q.chunk_rows = s.chunk_rows;
+  q.part_max = scale ? reinterpret_cast<uint32_t*>(ws + s.max_at) : nullptr;
+  q.part_sum = sum ? reinterpret_cast<float*>(ws + s.sum_at) : nullptr;
+  q.col_max = reinterpret_cast<float*>(ws + s.inv_at);
+  q.col_sum = sum;
+}
+
+int quantize_rows(const QuantizeArgs& q, uint32_t type, hipStream_t st) {
+  ScopedTiming tm("quantize_rows", st);
+  return status(launch_quantize_rows(q, type, st));
+}
+int quantize_columns(const QuantizeArgs& q, uint32_t type, hipStream_t st) {
+  {
+    ScopedTiming tm("column_max", st);
+    if (int rc = status(launch_column_max(q, type, st))) return rc;
+  }
+  if (!q.col_scale || !q.rows) return QSGD_OK;
+  ScopedTiming tm("quantize_columns", st);
+  return status(launch_quantize_columns(q, type, st));
+}
+
+// ---- product ---------------------------------------------------------------------
+
+constexpr uint64_t kMostLd = 1ull << 23;
+constexpr uint64_t kMostResults = 1ull << 42;   // of one product: its tiles are counted in 31 bits
+
+int product(ProductArgs& p, uint8_t* ws, hipStream_t st) {
+  const ProductPlan plan = plan_product(p.M, p.N, p.K);
+  p.splits = plan.splits; p.split_k = plan.split_k;
+  p.part = plan.bytes ? reinterpret_cast<int32_t*>(ws) : nullptr;
+  {
+    ScopedTiming tm("product", st);
+    if (int rc = status(launch_product(p, st))) return rc;
+  }
+  if (!p.part) return QSGD_OK;
+  ScopedTiming tm("product_join", st);
+  return status(launch_product_join(p, st));
+}
+
+bool too_many(uint64_t M, uint64_t N) { return N && M >= kMostResults / N; }
+
+uint64_t levels_ld(uint64_t k) { return (k + 15) / 16 * 16; }
+
+bool in_range(uint64_t a, uint64_t b, uint64_t c) { return a < 1ull << 31 && b < 1ull << 31 && c < 1ull << 31; }
+
+uint64_t product_bytes(uint64_t M, uint64_t N, uint64_t K) {
+  if (!M || !N || M >= kMostResults / N || K >= kMostLd) return 0;   // (nothing to do, or refused)
+  return plan_product((uint32_t)M, (uint32_t)N, (uint32_t)K).bytes;
+}
+
+bool room(const void* ws, size_t have, uint64_t need) { return need == 0 || (ws && aligned(ws, 16) && have >= need); }
+
+// Why a workspace is refused.
+int no_room(const void* ws, uint64_t need) { return need && (!ws || !aligned(ws, 16)) ? QSGD_ERR_INVALID_ARG : QSGD_ERR_CAPACITY; }
+
+// Workspace of the layer's gradients: levels and scales of its operands, then what their making and the products need,
+// one after the other.
+struct BackwardSpace {
+  uint64_t dy_rows, dy_row_scale, w_cols, w_scale, dy_cols, dy_col_scale, x_cols, x_scale, rest, bytes;
+};
+BackwardSpace backward_space(uint64_t M, uint64_t N, uint64_t K) {
+  BackwardSpace s = {};
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) { const uint64_t p = at; at += padded(bytes); return p; };
+  s.dy_rows = take(M * levels_ld(N)); s.dy_row_scale = take(4 * M);
+  s.w_cols = take(K * levels_ld(N)); s.w_scale = take(4 * K);
+  s.dy_cols = take(N * levels_ld(M)); s.dy_col_scale = take(4 * N);
+  s.x_cols = take(K * levels_ld(M)); s.x_scale = take(4 * K);
+  s.rest = at;
+  uint64_t rest = std::max(product_bytes(M, K, N), product_bytes(N, K, M));
+  for (const auto& [r, c] : {std::pair{M, N}, std::pair{N, K}, std::pair{M, K}}) rest = std::max(rest, column_space(r, c).bytes);
+  s.bytes = at + padded(rest);
+  return s;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qsgd_dropout(const qsgd_draws* draws, float p, const qsgd_matrix* x, const qsgd_matrix* residual, const qsgd_matrix* y,
+                 void* hip_stream) {
+  return dropout(draws, p, x, residual, y, "dropout", reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+int qsgd_dropout_backward(const qsgd_draws* draws, float p, const qsgd_matrix* dy, const qsgd_matrix* dx, void* hip_stream) {
+  return dropout(draws, p, dy, nullptr, dx, "dropout_backward", reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+size_t qsgd_quantize_workspace_bytes(uint64_t rows, uint64_t cols) {
+  return in_range(rows, cols, 0) && cols ? column_space(rows, cols).bytes : 0;
+}
+
+int qsgd_quantize(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix* x, const qsgd_matrix* rows,
+                  float* row_scale_dev, const qsgd_matrix* columns, float* column_scale_dev, void* workspace_dev,
+                  size_t workspace_bytes, void* hip_stream) {
+  if (rounding > QSGD_ROUND_STOCHASTIC || !sound(x, false) || (!rows && !columns)) return QSGD_ERR_INVALID_ARG;
+  if (rows && (!sound(rows, true) || !shaped(rows, x->rows, x->cols) || !floats(row_scale_dev, x->rows) || overlap(x, rows)))
+    return QSGD_ERR_INVALID_ARG;
+  if (columns && (!sound(columns, true) || !shaped(columns, x->cols, x->rows) || !floats(column_scale_dev, x->cols) ||
+                  overlap(x, columns) || (rows && overlap(rows, columns))))
+    return QSGD_ERR_INVALID_ARG;
+  QuantizeArgs q = {};
+  DrawArgs d = {};
+  if (rounding == QSGD_ROUND_STOCHASTIC || draws)
+    if (int rc = draw_args(draws, x->rows, d)) return rc;
+  const uint64_t need = columns ? qsgd_quantize_workspace_bytes(x->rows, x->cols) : 0;
+  if (!room(workspace_dev, workspace_bytes, need)) return no_room(workspace_dev, need);
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  fill(q, x, d, rounding == QSGD_ROUND_STOCHASTIC);
+  if (rows && x->rows) {
+    q.q_rows = reinterpret_cast<int8_t*>(rows->data_dev); q.q_rows_ld = rows->ld; q.row_scale = row_scale_dev;
+    if (int rc = quantize_rows(q, x->type, st)) return rc;
+  }
+  if (columns && x->cols) {
+    const ColumnSpace s = column_space(x->rows, x->cols);
+    fill_columns(q, s, reinterpret_cast<uint8_t*>(workspace_dev), reinterpret_cast<int8_t*>(columns->data_dev), columns->ld,
+                 column_scale_dev, nullptr);
+    if (int rc = quantize_columns(q, x->type, st)) return rc;
+  }
+  return QSGD_OK;
+}
+
+size_t qsgd_int_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
+  return in_range(M, N, K) ? product_bytes(M, N, K) : 0;
+}
+
+int qsgd_int_matmul(const qsgd_matrix* a, const float* a_scale_dev, const qsgd_matrix* b, const float* b_scale_dev,
+                    const float* bias_dev, const qsgd_matrix* y, void* workspace_dev, size_t workspace_bytes,
+                    void* hip_stream) {
+  if (!sound(a, true) || !sound(b, true) || !sound(y, false) || a->cols != b->cols || !shaped(y, a->rows, b->rows) ||
+      !floats(a_scale_dev, a->rows) || !floats(b_scale_dev, b->rows) || !aligned(bias_dev, 4) || overlap(a, y) || overlap(b, y))
+    return QSGD_ERR_INVALID_ARG;
+  if (a->ld >= kMostLd || b->ld >= kMostLd || too_many(y->rows, y->cols)) return QSGD_ERR_UNSUPPORTED;
+  if (y->rows == 0 || y->cols == 0) return QSGD_OK;
+  const uint64_t need = product_bytes(a->rows, b->rows, a->cols);
+  if (!room(workspace_dev, workspace_bytes, need)) return no_room(workspace_dev, need);
+  ProductArgs p = {};
+  p.a = reinterpret_cast<const int8_t*>(a->data_dev); p.a_ld = a->ld;
+  p.b = reinterpret_cast<const int8_t*>(b->data_dev); p.b_ld = b->ld;
+  p.M = (uint32_t)a->rows; p.N = (uint32_t)b->rows; p.K = (uint32_t)a->cols;
+  p.a_scale = a_scale_dev; p.b_scale = b_scale_dev; p.bias = bias_dev;
+  p.y = y->data_dev; p.y_ld = y->ld; p.type = y->type;
+  return product(p, reinterpret_cast<uint8_t*>(workspace_dev), reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+size_t qsgd_linear_forward_workspace_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs) {
+  if (!in_range(tokens, outputs, inputs)) return 0;
+  return padded(tokens * levels_ld(inputs)) + padded(4 * tokens) + product_bytes(tokens, outputs, inputs);
+}
+
+int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix* x, const qsgd_matrix* w,
+                        const float* w_scale_dev, const float* bias_dev, const qsgd_matrix* y, void* workspace_dev,
+                        size_t workspace_bytes, void* hip_stream) {
+  if (rounding > QSGD_ROUND_STOCHASTIC || !sound(x, false) || !sound(w, true) || !sound(y, false) || x->cols != w->cols ||
+      !shaped(y, x->rows, w->rows) || y->type != x->type || !floats(w_scale_dev, w->rows) || !aligned(bias_dev, 4) ||
+      overlap(x, y) || overlap(w, y))
+    return QSGD_ERR_INVALID_ARG;
+  if (w->ld >= kMostLd || levels_ld(x->cols) >= kMostLd || too_many(y->rows, y->cols)) return QSGD_ERR_UNSUPPORTED;
+  QuantizeArgs q = {};
+  DrawArgs d = {};
+  if (rounding == QSGD_ROUND_STOCHASTIC || draws)
+    if (int rc = draw_args(draws, x->rows, d)) return rc;
+  if (y->rows == 0 || y->cols == 0) return QSGD_OK;
+  const uint64_t need = qsgd_linear_forward_workspace_bytes(x->rows, w->rows, x->cols);
+  if (!room(workspace_dev, workspace_bytes, need)) return no_room(workspace_dev, need);
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  uint8_t* ws = reinterpret_cast<uint8_t*>(workspace_dev);
+  const uint64_t ld = levels_ld(x->cols), scale_at = padded(x->rows * ld), rest = scale_at + padded(4 * x->rows);
+  fill(q, x, d, rounding == QSGD_ROUND_STOCHASTIC);
+  q.q_rows = reinterpret_cast<int8_t*>(ws); q.q_rows_ld = ld; q.row_scale = reinterpret_cast<float*>(ws + scale_at);
+  if (int rc = quantize_rows(q, x->type, st)) return rc;
+  ProductArgs p = {};
+  p.a = q.q_rows; p.a_ld = ld;
+  p.b = reinterpret_cast<const int8_t*>(w->data_dev); p.b_ld = w->ld;
+  p.M = (uint32_t)x->rows; p.N = (uint32_t)w->rows; p.K = (uint32_t)x->cols;
+  p.a_scale = q.row_scale; p.b_scale = w_scale_dev; p.bias = bias_dev;
+  p.y = y->data_dev; p.y_ld = y->ld; p.type = y->type;
+  return product(p, ws + rest, st);
+}
+
+size_t qsgd_linear_backward_workspace_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs) {
+  if (!in_range(tokens, outputs, inputs) || tokens >= kMostLd || outputs >= kMostLd) return 0;
+  return backward_space(tokens, outputs, inputs).bytes;
+}
+
+int qsgd_linear_backward(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix* x, const qsgd_matrix* w,
+                         const qsgd_matrix* dy, const qsgd_matrix* dx, const qsgd_matrix* dw, float* db_dev,
+                         void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  if (rounding > QSGD_ROUND_STOCHASTIC || !sound(x, false) || !sound(w, false) || !sound(dy, false) || x->cols != w->cols ||
+      !shaped(dy, x->rows, w->rows) || w->type != x->type || dy->type != x->type || (!dx && !dw && !db_dev) ||
+      !aligned(db_dev, 4))
+    return QSGD_ERR_INVALID_ARG;
+  const qsgd_matrix *in[3] = {x, w, dy}, *out[2] = {dx, dw};
+  if (dx && (!sound(dx, false) || !shaped(dx, x->rows, x->cols) || dx->type != x->type)) return QSGD_ERR_INVALID_ARG;
+  if (dw && (!sound(dw, false) || !shaped(dw, w->rows, w->cols) || dw->type != QSGD_TYPE_F32)) return QSGD_ERR_INVALID_ARG;
+  for (const auto* o : out)
+    for (const auto* i : in)
+      if (o && overlap(o, i)) return QSGD_ERR_INVALID_ARG;
+  if (dx && dw && overlap(dx, dw)) return QSGD_ERR_INVALID_ARG;
+  const uint64_t M = x->rows, N = w->rows, K = x->cols;
+  if (levels_ld(N) >= kMostLd || levels_ld(M) >= kMostLd || too_many(M, K) || too_many(N, K)) return QSGD_ERR_UNSUPPORTED;
+  QuantizeArgs base = {};
+  DrawArgs d = {};
+  if (rounding == QSGD_ROUND_STOCHASTIC || draws) {
+    if (int rc = draw_args(draws, M, d)) return rc;
+  }
+  const BackwardSpace s = backward_space(M, N, K);
+  if (!room(workspace_dev, workspace_bytes, s.bytes)) return no_room(workspace_dev, s.bytes);
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  uint8_t* ws = reinterpret_cast<uint8_t*>(workspace_dev);
+  auto levels = [&](uint64_t at) { return reinterpret_cast<int8_t*>(ws + at); };
+  auto scales = [&](uint64_t at) { return reinterpret_cast<float*>(ws + at); };
+  DrawArgs draws_w = d, draws_x = d;
+  draws_w.stream_id += 1; draws_w.row_base = 0;
+  draws_x.stream_id += 2;
+  const bool stochastic = rounding == QSGD_ROUND_STOCHASTIC;
+  const bool want_dx = dx && M && K, want_dw = dw && N && K;
+  if ((want_dw || db_dev) && N) {   // dy by columns, and its sums
+    fill(base, dy, d, stochastic);
+    fill_columns(base, column_space(M, N), ws + s.rest, levels(s.dy_cols), levels_ld(M),
+                 want_dw ? scales(s.dy_col_scale) : nullptr, db_dev);
+    if (int rc = quantize_columns(base, dy->type, st)) return rc;
+  }
+  if (want_dw) {
+    QuantizeArgs q = {};
+    fill(q, x, draws_x, stochastic);
+    fill_columns(q, column_space(M, K), ws + s.rest, levels(s.x_cols), levels_ld(M), scales(s.x_scale), nullptr);
+    if (int rc = quantize_columns(q, x->type, st)) return rc;
+    ProductArgs p = {};
+    p.a = levels(s.dy_cols); p.b = levels(s.x_cols); p.a_ld = p.b_ld = levels_ld(M);
+    p.M = (uint32_t)N; p.N = (uint32_t)K; p.K = (uint32_t)M;
+    p.a_scale = scales(s.dy_col_scale); p.b_scale = scales(s.x_scale);
+    p.y = dw->data_dev; p.y_ld = dw->ld; p.type = QSGD_TYPE_F32;
+    if (int rc = product(p, ws + s.rest, st)) return rc;
+  }
+  if (want_dx) {
+    QuantizeArgs r = {}, q = {};
+    fill(r, dy, d, stochastic);
+    r.q_rows = levels(s.dy_rows); r.q_rows_ld = levels_ld(N); r.row_scale = scales(s.dy_row_scale);
+    if (int rc = quantize_rows(r, dy->type, st)) return rc;
+    fill(q, w, draws_w, stochastic);
+    fill_columns(q, column_space(N, K), ws + s.rest, levels(s.w_cols), levels_ld(N), scales(s.w_scale), nullptr);
+    if (int rc = quantize_columns(q, w->type, st)) return rc;
+    ProductArgs p = {};
+    p.a = levels(s.dy_rows); p.b = levels(s.w_cols); p.a_ld = p.b_ld = levels_ld(N);
+    p.M = (uint32_t)M; p.N = (uint32_t)K; p.K = (uint32_t)N;
+    p.a_scale = scales(s.dy_row_scale); p.b_scale = scales(s.w_scale);
+    p.y = dx->data_dev; p.y_ld = dx->ld; p.type = dx->type;
+    if (int rc = product(p, ws + s.rest, st)) return rc;
+  }
+  return QSGD_OK;
+}
+
+}  // extern "C"
