@@ -143,6 +143,7 @@ int product(ProductArgs& p, uint8_t* ws, hipStream_t st) {
   const ProductPlan plan = plan_product(p.M, p.N, p.K);
   p.splits = plan.splits; p.split_k = plan.split_k;
   p.part = plan.bytes ? reinterpret_cast<int32_t*>(ws) : nullptr;
+  p.wide = p.part ? p.N % 4 == 0 : aligned(p.y, 16) && (p.M <= 1 || p.y_ld * size_of(p.type) % 16 == 0);
   {
     ScopedTiming tm("product", st);
     if (int rc = status(launch_product(p, st))) return rc;

@@ -147,6 +147,7 @@ struct ProductArgs {
   void* y;
   uint64_t y_ld;
   uint32_t type;
+  bool wide;                  // what is written (y, or the sums) has rows aligned to 16 bytes
   uint32_t splits, split_k;   // pieces of K and their length (a multiple of the tile's depth)
   int32_t* part;              // splits x M x N sums, or null with one piece
 };
