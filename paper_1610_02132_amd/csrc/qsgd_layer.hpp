@@ -42,11 +42,17 @@ template <> struct Element<QSGD_TYPE_BF16> {
   using bits = uint16_t;
   __device__ static float widen(uint32_t b) { return __uint_as_float(b << 16); }
   __device__ static uint32_t narrow(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+  __device__ static uint32_t narrow2(float v, float w) {   // two values in a word
+    using values = __attribute__((ext_vector_type(2))) float;
+    using pair = __attribute__((ext_vector_type(2))) __bf16;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((values{v, w}), pair));
+  }
 };
 template <> struct Element<QSGD_TYPE_F16> {
   using bits = uint16_t;
   __device__ static float widen(uint32_t b) { return (float)__builtin_bit_cast(_Float16, (uint16_t)b); }
   __device__ static uint32_t narrow(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+  __device__ static uint32_t narrow2(float v, float w) { return narrow(v) | narrow(w) << 16; }
 };
 
 // Eight neighbouring elements: 16 bytes of a 16-bit type, 32 of fp32.
@@ -151,9 +157,16 @@ struct ProductArgs {
   uint32_t splits, split_k;   // pieces of K and their length (a multiple of the tile's depth)
   int32_t* part;              // splits x M x N sums, or null with one piece
 };
-struct ProductPlan { uint32_t splits, split_k; uint64_t bytes; };
+enum ProductKind : uint32_t {
+  kProductFew,        // at most 64 rows of a, straight from memory
+  kProductTile64Deep, // tiles of 64 x 64 results, four stages of k, ...
+  kProductTile64,     // ... and two
+  kProductTile128,
+  kProductTile256,
+};
+struct ProductPlan { uint32_t kind, splits, split_k; uint64_t bytes; };
 ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K);
-hipError_t launch_product(const ProductArgs& a, hipStream_t st);
+hipError_t launch_product(const ProductArgs& a, uint32_t kind, hipStream_t st);
 hipError_t launch_product_join(const ProductArgs& a, hipStream_t st);
 
 }  // namespace qsgd

@@ -2,6 +2,9 @@
 //   y[m][n] = (sum_k a[m][k] b[n][k]) a_scale[m] b_scale[n] + bias[n],
 // both operands with k contiguous.  The sum is an integer and exact whatever the order, so that pieces of k
 // can be summed apart (a workspace of int32 sums, joined in 64 bits) without changing the result.
+#include <algorithm>
+#include <cmath>
+
 #include "qsgd_layer.hpp"
 
 namespace qsgd {
@@ -10,49 +13,51 @@ namespace {
 using int4v = __attribute__((ext_vector_type(4))) int;
 using int16v = __attribute__((ext_vector_type(16))) int;
 
-// Most of k in one piece: 131008 * 128 * 128 < 2^31.
-constexpr uint32_t kMostK = 131008;
+// Most of k in one piece: 130816 * 128 * 128 < 2^31, and a multiple of 256.
+constexpr uint32_t kMostK = 130816;
 constexpr uint32_t kSums = 99;   // "type" of a piece's sums in the workspace
 
-// The sum times both scales, the smaller one first: an intermediate result overflows or vanishes only
-// where the result does.  (A scale that is NaN compares false and stays.)
-__device__ __forceinline__ float scaled(float sum, float s, float t) {
-  const float lo = s < t ? s : t, hi = s < t ? t : s;
-  return sum * lo * hi;
+// The sum times the row's scale, times the column's, plus the bias, the last two in one rounding.  A row's scale above
+// kBigScale is taken 2^64 times smaller and the product larger again, so that a result overflows only where it has to;
+// the sum is a whole number and the scales are not subnormal, so that nothing vanishes on the way.
+constexpr float kBigScale = 0x1p96f;
+__device__ __forceinline__ float result(float sum, float s, float t, float bias) {
+  return s > kBigScale ? sum * (s * 0x1p-64f) * t * 0x1p64f + bias : __builtin_fmaf(sum * s, t, bias);
 }
 
 template <uint32_t TYPE>
-__device__ __forceinline__ void put(const ProductArgs& a, uint32_t m, uint32_t n, float v) {
-  if (a.bias) v += a.bias[n];
+__device__ __forceinline__ void put(const ProductArgs& a, uint32_t m, uint32_t n, float sum) {
+  const float v = result(sum, a.a_scale[m], a.b_scale[n], a.bias ? a.bias[n] : 0.0f);
   *reinterpret_cast<typename Element<TYPE>::bits*>(element_at<TYPE>(a.y, a.y_ld, m, n)) =
       (typename Element<TYPE>::bits)Element<TYPE>::narrow(v);
 }
 
-// 16 bytes of an operand's row from k on; the row is clamped into the matrix (its results are not
-// written), k into the row, where bytes behind K are zeroed in one of the operands.
-__device__ __forceinline__ uint4 operand(const int8_t* p, uint64_t ld, uint32_t row, uint32_t rows, uint32_t k,
-                                         uint32_t K, bool mask) {
-  const uint32_t last = (K + 15) / 16 * 16 - 16, at = min(k, last);
-  uint4 v = *reinterpret_cast<const uint4*>(p + (min(row, rows - 1) * ld + at));
-  if (mask && k + 16 > K) {
-    const uint32_t n = k < K ? K - k : 0u;   // valid bytes
-    uint32_t* w = &v.x;
+// 16 bytes of an operand from k on, those behind K zeroed.
+__device__ __forceinline__ int4v masked(int4v v, uint32_t k, uint32_t K) {
+  const uint32_t n = k < K ? K - k : 0u;   // valid bytes
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
-      const uint32_t have = n > 4 * j ? min(n - 4 * j, 4u) : 0u;
-      w[j] &= have == 4 ? ~0u : (1u << (8 * have)) - 1u;
-    }
+  for (uint32_t j = 0; j < 4; ++j) {
+    const uint32_t have = n > 4 * j ? min(n - 4 * j, 4u) : 0u;
+    v[j] = have == 4 ? v[j] : (int)((uint32_t)v[j] & ((1u << (8 * have)) - 1u));
   }
   return v;
+}
+
+// ... of its row, straight from memory; the row is clamped into the matrix (its results are not written), k into the row.
+__device__ __forceinline__ int4v operand(const int8_t* p, uint64_t ld, uint32_t row, uint32_t rows, uint32_t k, uint32_t K) {
+  return *reinterpret_cast<const int4v*>(p + (min(row, rows - 1) * ld + min(k, (K + 15) / 16 * 16 - 16)));
 }
 
 // ---- tiles ------------------------------------------------------------------------
 // A workgroup of four wavefronts makes a tile of 64 MI x 64 NI results, each wavefront 32 MI x 32 NI of them in
 // registers (MFMA 32x32x32: the weights' rows are the rows, so that a lane holds four neighbouring results of
-// one row of y).  64 bytes of k are a stage; four stages are in LDS, loaded straight from memory three and a half
-// stages ahead.  Slot s of a row of 64 bytes holds chunk s ^ (row / 2 % 4), which spreads the 16-byte reads
-// of eight rows over all banks.
-constexpr uint32_t kDepth = 64;   // bytes of k in a stage
+// one row of y).  128 bytes of k, whole cache lines, are a stage; STAGES of them are in LDS, loaded straight from memory.
+// Slot s of a row of 128 bytes holds chunk s ^ swizzle(row).
+constexpr uint32_t kDepth = 128;   // bytes of k in a stage
+
+// Rows whose 16-byte chunks of one number are read together (8 or 16 neighbours, or fours of them whose numbers differ
+// in bits 2 and 3) get places in different banks: by bits 1, 2 and 3 where bit 0 is equal, and by bits 0, 1 and 2.
+__device__ __forceinline__ uint32_t swizzle(uint32_t row) { return (row >> 1 & 3) | ((row ^ row >> 3) & 1) << 2; }
 
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t* to, uint32_t voffset, uint32_t soffset) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, voffset, soffset, 0, 0);
@@ -90,241 +95,387 @@ __device__ __forceinline__ void weave() {
 #pragma unroll
   for (int i = 0; i < READS; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);               // reads of LDS
-    if (LOADS) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);     // loads
+    if (LOADS) __builtin_amdgcn_sched_group_barrier(0x20, LOADS / READS, 0);   // loads
     __builtin_amdgcn_sched_group_barrier(0x8, kEach, 0);             // matrix instructions
   }
   __builtin_amdgcn_sched_barrier(0);
 }
 
-template <int MI, int NI, uint32_t TYPE>
+template <int MI, int NI, int STAGES, uint32_t TYPE>
 __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductArgs a) {
   constexpr uint32_t TM = 64 * MI, TN = 64 * NI, kStage = (TM + TN) * kDepth;
-  constexpr int kLoads = MI + NI;   // of a wavefront and stage, 16 rows each
-  __shared__ __attribute__((aligned(16))) uint8_t s0[kStage], s1[kStage], s2[kStage], s3[kStage];
+  constexpr int kLoads = 2 * (MI + NI);   // of a wavefront and stage, 8 rows each
+  __shared__ __attribute__((aligned(16))) uint8_t s0[kStage], s1[kStage], s2[STAGES > 2 ? kStage : 16], s3[STAGES > 3 ? kStage : 16];
   uint32_t tm, tn;
   place_tile(blockIdx.x, (a.M + TM - 1) / TM, (a.N + TN - 1) / TN, tm, tn);
   const uint32_t m0 = tm * TM, n0 = tn * TN;
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t k0 = blockIdx.y * a.split_k, k1 = min(k0 + a.split_k, a.K);
-  const uint32_t steps = (k1 - k0) / kDepth;
-  const uint32_t rows_a = min(TM, a.M - m0), rows_b = min(TN, a.N - n0);
-  const auto from_a = __builtin_amdgcn_make_buffer_rsrc((void*)(a.a + m0 * a.a_ld), 0, (int)((rows_a - 1) * (uint32_t)a.a_ld + (a.K + 15) / 16 * 16), 0x27000);
-  const auto from_b = __builtin_amdgcn_make_buffer_rsrc((void*)(a.b + n0 * a.b_ld), 0, (int)((rows_b - 1) * (uint32_t)a.b_ld + (a.K + 15) / 16 * 16), 0x27000);
-  uint32_t at_a[MI], at_b[NI];   // rows are clamped into the matrix
-  const uint32_t chunk = 16 * ((lane & 3) ^ (lane >> 3 & 3));
+  // stages, and those of them that k fills; the last may be a part
+  const uint32_t steps = (k1 - k0 + kDepth - 1) / kDepth, whole = (k1 - k0) / kDepth;
+  const uint32_t rows_a = min(TM, a.M - m0), rows_b = min(TN, a.N - n0), padded = (a.K + 15) / 16 * 16;
+  const auto from_a = __builtin_amdgcn_make_buffer_rsrc((void*)(a.a + m0 * a.a_ld), 0, (int)((rows_a - 1) * (uint32_t)a.a_ld + padded), 0x27000);
+  const auto from_b = __builtin_amdgcn_make_buffer_rsrc((void*)(a.b + n0 * a.b_ld), 0, (int)((rows_b - 1) * (uint32_t)a.b_ld + padded), 0x27000);
+  uint32_t at_a[2 * MI], at_b[2 * NI];   // rows are clamped into the matrix
+  auto chunk = [&](int i) { return 16 * ((lane & 7) ^ swizzle((lane >> 3) + 8 * (i & 1))); };
 #pragma unroll
-  for (int i = 0; i < MI; ++i) at_a[i] = min(16u * (MI * wave + i) + (lane >> 2), rows_a - 1) * (uint32_t)a.a_ld + chunk;
+  for (int i = 0; i < 2 * MI; ++i) at_a[i] = min(8u * (2 * MI * wave + i) + (lane >> 3), rows_a - 1) * (uint32_t)a.a_ld + chunk(i);
 #pragma unroll
-  for (int i = 0; i < NI; ++i) at_b[i] = min(16u * (NI * wave + i) + (lane >> 2), rows_b - 1) * (uint32_t)a.b_ld + chunk;
-  auto load = [&](uint32_t step, uint8_t* to) {
-    const uint32_t k = k0 + step * kDepth;
+  for (int i = 0; i < 2 * NI; ++i) at_b[i] = min(8u * (2 * NI * wave + i) + (lane >> 3), rows_b - 1) * (uint32_t)a.b_ld + chunk(i);
+  // Loads [from, to) of a stage; the last stage may be a part, whose chunks are clamped into the row.
+  auto load = [&](uint32_t step, uint8_t* place, int from, int to, bool last) {
+    const uint32_t k = k0 + step * kDepth, end = padded - 16 - k;
+    auto clamped = [&](uint32_t at, int i) { return last && step >= whole ? at - chunk(i) + min(chunk(i), end) : at; };
 #pragma unroll
-    for (int i = 0; i < MI; ++i) load_to_lds(from_a, to + 1024 * (MI * wave + i), at_a[i], k);
+    for (int i = 0; i < 2 * MI; ++i)
+      if (i >= from && i < to) load_to_lds(from_a, place + 1024 * (2 * MI * wave + i), clamped(at_a[i], i), k);
 #pragma unroll
-    for (int i = 0; i < NI; ++i) load_to_lds(from_b, to + TM * kDepth + 1024 * (NI * wave + i), at_b[i], k);
+    for (int i = 0; i < 2 * NI; ++i)
+      if (2 * MI + i >= from && 2 * MI + i < to)
+        load_to_lds(from_b, place + TM * kDepth + 1024 * (2 * NI * wave + i), clamped(at_b[i], i), k);
   };
   const uint32_t wm = (wave & 1) * 32 * MI, wn = (wave >> 1) * 32 * NI;   // the wavefront's part of the tile
-  const uint32_t frag = (lane & 31) * kDepth + 16 * ((lane >> 5) ^ (lane >> 1 & 3));
+  const uint32_t frag = (lane & 31) * kDepth + 16 * ((lane >> 5) ^ swizzle(lane));
   int4v xf[2][MI], wf[2][NI];
-  auto read = [&](const uint8_t* from, int half) {
+  auto read = [&](const uint8_t* from, int quarter) {
 #pragma unroll
     for (int i = 0; i < NI; ++i)
-      wf[half][i] = *reinterpret_cast<const int4v*>(from + (TM + wn + 32 * i) * kDepth + (frag ^ (32 * half)));
+      wf[quarter & 1][i] = *reinterpret_cast<const int4v*>(from + (TM + wn + 32 * i) * kDepth + (frag ^ (32 * quarter)));
 #pragma unroll
     for (int i = 0; i < MI; ++i)
-      xf[half][i] = *reinterpret_cast<const int4v*>(from + (wm + 32 * i) * kDepth + (frag ^ (32 * half)));
+      xf[quarter & 1][i] = *reinterpret_cast<const int4v*>(from + (wm + 32 * i) * kDepth + (frag ^ (32 * quarter)));
   };
   int16v acc[MI][NI] = {};
-  auto multiply = [&](int half) {
+  auto multiply = [&](int quarter) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[half][j], xf[half][i], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < NI; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[quarter & 1][j], xf[quarter & 1][i], acc[i][j], 0, 0, 0);
   };
-  // Stage `now` has its first half in registers when its step begins.  Behind the barrier all wavefronts have read
-  // the stage and hold the next one's loads: its place is loaded again.
-  auto step = [&](uint8_t* now, const uint8_t* next, uint32_t s) {
+  // Stage `now` has its first quarter in registers when its step begins.  Behind the barrier all wavefronts have read
+  // the stage and hold the next one's loads: its place is loaded again, one part of the loads with the last quarter and
+  // one with the next step's first (`prior` is the stage before), as they come faster than they are taken.
+  constexpr int kPart = kLoads / 2;
+  auto step = [&](uint8_t* now, const uint8_t* next, uint8_t* prior, uint32_t s) {
+    load(s + STAGES - 1, prior, kPart, kLoads, false);
     read(now, 1);
     multiply(0);
-    weave<MI * NI, MI + NI, 0>();
-    wait_loads<2 * kLoads>();
-    meet();
-    load(s + 4, now);
-    read(next, 0);
+    weave<MI * NI, MI + NI, (kLoads - kPart)>();
+    read(now, 2);
     multiply(1);
-    weave<MI * NI, MI + NI, MI + NI>();
+    weave<MI * NI, MI + NI, 0>();
+    read(now, 3);
+    multiply(2);
+    weave<MI * NI, MI + NI, 0>();
+    wait_loads<(STAGES - 2) * kLoads>();
+    meet();
+    load(s + STAGES, now, 0, kPart, false);
+    read(next, 0);
+    multiply(3);
+    weave<MI * NI, MI + NI, kPart>();
   };
-  auto last_step = [&](uint8_t* now, const uint8_t* next, uint32_t s) {   // ... of the last seven, where loads end
+  auto last_step = [&](uint8_t* now, const uint8_t* next, uint8_t* prior, uint32_t s) {   // ... of the last ones, where loads end
+    if (s + STAGES - 1 < steps) load(s + STAGES - 1, prior, kPart, kLoads, true);
     read(now, 1);
     multiply(0);
     weave<MI * NI, MI + NI, 0>();
-    if (s + 3 < steps) wait_loads<2 * kLoads>();
-    else if (s + 2 < steps) wait_loads<kLoads>();
+    read(now, 2);
+    multiply(1);
+    weave<MI * NI, MI + NI, 0>();
+    read(now, 3);
+    multiply(2);
+    weave<MI * NI, MI + NI, 0>();
+    if (STAGES > 3 && s + 3 < steps) wait_loads<(STAGES - 2) * kLoads>();
+    else if (STAGES > 2 && s + 2 < steps) wait_loads<kLoads>();
     else wait_loads<0>();
     meet();
-    if (s + 4 < steps) load(s + 4, now);
+    if (s + STAGES < steps) load(s + STAGES, now, 0, kPart, true);
     read(next, 0);
-    multiply(1);
+    multiply(3);
   };
+  static_assert(STAGES == 2 || STAGES == 4, "");
   if (steps > 0) {
-    load(0, s0);
-    if (steps > 1) load(1, s1);
-    if (steps > 2) load(2, s2);
-    if (steps > 3) { load(3, s3); wait_loads<3 * kLoads>(); }
-    else if (steps > 2) wait_loads<2 * kLoads>();
-    else if (steps > 1) wait_loads<kLoads>();
+    load(0, s0, 0, kLoads, true);
+    if (steps > 1) load(1, s1, 0, STAGES > 2 ? kLoads : kPart, true);
+    if (STAGES > 2 && steps > 2) load(2, s2, 0, kLoads, true);
+    if (STAGES > 2 && steps > 3) { load(3, s3, 0, kPart, true); wait_loads<(2 * kLoads + kPart)>(); }
+    else if (STAGES > 2 && steps > 2) wait_loads<2 * kLoads>();
+    else if (steps > 1) wait_loads<(STAGES > 2 ? kLoads : kPart)>();
     else wait_loads<0>();
     meet();
     read(s0, 0);
     uint32_t s = 0;
-    for (; s + 8 <= steps; s += 4) {
-      step(s0, s1, s);
-      step(s1, s2, s + 1);
-      step(s2, s3, s + 2);
-      step(s3, s0, s + 3);
+    for (; s + 2 * STAGES <= whole; s += STAGES) {
+      if constexpr (STAGES == 2) {
+        step(s0, s1, s1, s);
+        step(s1, s0, s0, s + 1);
+      } else {
+        step(s0, s1, s3, s);
+        step(s1, s2, s0, s + 1);
+        step(s2, s3, s1, s + 2);
+        step(s3, s0, s2, s + 3);
+      }
     }
-    for (; s < steps; s += 4) {
-      last_step(s0, s1, s);
-      if (s + 1 >= steps) break;
-      last_step(s1, s2, s + 1);
-      if (s + 2 >= steps) break;
-      last_step(s2, s3, s + 2);
-      if (s + 3 >= steps) break;
-      last_step(s3, s0, s + 3);
+    for (; s < whole; s += STAGES) {
+      last_step(s0, s1, STAGES == 2 ? s1 : s3, s);
+      if (s + 1 >= whole) break;
+      last_step(s1, STAGES == 2 ? s0 : s2, s0, s + 1);
+      if (STAGES == 2) continue;
+      if (s + 2 >= whole) break;
+      last_step(s2, s3, s1, s + 2);
+      if (s + 3 >= whole) break;
+      last_step(s3, s0, s2, s + 3);
     }
-  }
-  if (k0 + steps * kDepth < k1) {   // what is left of k, less than a stage: straight from memory, masked
+    if (whole < steps) {   // the part: what lies behind K counts as zero in one of the operands
+      const uint32_t at = whole % STAGES;
+      const uint8_t* now = at == 0 ? s0 : at == 1 ? s1 : at == 2 ? s2 : s3;
 #pragma unroll
-    for (uint32_t half = 0; half < 2; ++half) {
-      const uint32_t k = k0 + steps * kDepth + 32 * half + 16 * (lane >> 5);
+      for (int q = 0; q < 4; ++q) {
+        read(now, q);
+        const uint32_t k = k0 + whole * kDepth + 32 * q + 16 * (lane >> 5);
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
-        xf[0][i] = __builtin_bit_cast(int4v, operand(a.a, a.a_ld, m0 + wm + 32 * i + (lane & 31), a.M, k, a.K, true));
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-        wf[0][i] = __builtin_bit_cast(int4v, operand(a.b, a.b_ld, n0 + wn + 32 * i + (lane & 31), a.N, k, a.K, false));
-      multiply(0);
+        for (int i = 0; i < MI; ++i) xf[q & 1][i] = masked(xf[q & 1][i], k, a.K);
+        multiply(q);
+      }
     }
   }
   // The results leave through LDS, 32 rows of the wavefront's part at a time, so that a store covers whole lines.
   meet();   // (all wavefronts have read their last stage)
-  constexpr uint32_t kSize = TYPE == QSGD_TYPE_F32 || TYPE == kSums ? 4 : 2;
-  constexpr uint32_t kRow = 32 * NI * kSize + 16, kPer = 16 / kSize, kChunks = 32 * NI / kPer;   // bytes, results of 16 bytes, of which a row has
-  constexpr uint32_t kBlock = 32 * kRow;                // then the part's scales and biases
-  static_assert(kBlock + 2 * 32 * NI * 4 <= kStage, "");
-  uint8_t* stage = wave == 0 ? s0 : wave == 1 ? s1 : wave == 2 ? s2 : s3;
-  float* w_scale = reinterpret_cast<float*>(stage + kBlock);
-  float* bias = w_scale + 32 * NI;
+  constexpr uint32_t kSize = TYPE == QSGD_TYPE_F32 || TYPE == kSums ? 4 : 2, kPer = 16 / kSize;   // results of 16 bytes
+  constexpr uint32_t kRow = 32 * NI * 4 + 16, kChunks = 32 * NI / kPer, kRows = 64 / kChunks;      // rows that a store covers
+  static_assert(32 * kRow + 32 * MI * 4 <= kStage / 2, "");
+  uint8_t* stage = (wave < 2 ? s0 : s1) + (wave & 1) * (kStage / 2);
+  float* x_scale = reinterpret_cast<float*>(stage + 32 * kRow);
+  const uint32_t n = n0 + wn + lane % kChunks * kPer;   // a lane's columns are the same for every row
+  float w_scale[kPer], bias[kPer];
+  bool big = false;   // any row's scale is
   if constexpr (TYPE != kSums) {
-    for (uint32_t j = lane; j < 32 * NI; j += 64) {
-      const uint32_t n = min(n0 + wn + j, a.N - 1);
-      w_scale[j] = a.b_scale[n];
-      bias[j] = a.bias ? a.bias[n] : 0.0f;
+#pragma unroll
+    for (uint32_t e = 0; e < kPer; ++e) {
+      const uint32_t at = min(n + e, a.N - 1);
+      w_scale[e] = a.b_scale[at];
+      bias[e] = a.bias ? a.bias[at] : 0.0f;
     }
+    for (uint32_t r = lane; r < 32 * MI; r += 64) {
+      x_scale[r] = a.a_scale[min(m0 + wm + r, a.M - 1)];
+      big |= x_scale[r] > kBigScale;
+    }
+    big = __any(big);
   }
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
-    const uint32_t row0 = m0 + wm + 32 * i;
-    float x_scale = 0.0f;
-    if constexpr (TYPE != kSums) x_scale = a.a_scale[min(row0 + (lane & 31), a.M - 1)];
 #pragma unroll
     for (int j = 0; j < NI; ++j)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        uint32_t w[4];
-        const float4 ws = *reinterpret_cast<const float4*>(w_scale + 32 * j + 8 * g + 4 * (lane >> 5));
-        const float4 bs = *reinterpret_cast<const float4*>(bias + 32 * j + 8 * g + 4 * (lane >> 5));
-        const float each[4] = {ws.x, ws.y, ws.z, ws.w}, plus[4] = {bs.x, bs.y, bs.z, bs.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int sum = acc[i][j][4 * g + e];
-          if constexpr (TYPE == kSums) w[e] = (uint32_t)sum;
-          else {
-            float v = scaled((float)sum, x_scale, each[e]);
-            if (a.bias) v += plus[e];
-            w[e] = Element<TYPE>::narrow(v);
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);   // (one group's values in registers at a time)
-        uint8_t* to = stage + (lane & 31) * kRow + (32 * j + 8 * g + 4 * (lane >> 5)) * kSize;
-        if constexpr (kSize == 4) *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-        else *reinterpret_cast<uint2*>(to) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
-      }
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<int4v*>(stage + (lane & 31) * kRow + (32 * j + 8 * g + 4 * (lane >> 5)) * 4) =
+            int4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
     wait_loads<63>();   // (the wavefront's writes have arrived)
-    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (uint32_t it = 0; it < kChunks / 2; ++it) {
-      const uint32_t c = 64 * it + lane;
-      const uint32_t row = c / kChunks, n = n0 + wn + c % kChunks * kPer, m = row0 + row;
-      const uint4 v = *reinterpret_cast<const uint4*>(stage + row * kRow + c % kChunks * 16);
-      if (m >= a.M || n >= a.N) continue;
-      uint8_t* out = TYPE == kSums ? reinterpret_cast<uint8_t*>(a.part) + (((uint64_t)blockIdx.y * a.M + m) * a.N + n) * 4
-                                   : reinterpret_cast<uint8_t*>(a.y) + (m * a.y_ld + n) * kSize;
-      if (a.wide && n + kPer <= a.N) {
-        *reinterpret_cast<uint4*>(out) = v;
+    for (uint32_t it = 0; it < 32 / kRows; ++it) {
+      const uint32_t row = it * kRows + lane / kChunks, m = m0 + wm + 32 * i + row;
+      const int4v* from = reinterpret_cast<const int4v*>(stage + row * kRow + lane % kChunks * kPer * 4);
+      uint4 out;
+      if constexpr (TYPE == kSums) {
+        out = __builtin_bit_cast(uint4, from[0]);
       } else {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        const float s = x_scale[32 * i + row];
+        float v[kPer];
+#pragma unroll
+        for (uint32_t e = 0; e < kPer; ++e) v[e] = __builtin_fmaf((float)from[e / 4][e % 4] * s, w_scale[e], bias[e]);
+        if (big) {
+#pragma unroll
+          for (uint32_t e = 0; e < kPer; ++e) v[e] = result((float)from[e / 4][e % 4], s, w_scale[e], bias[e]);
+        }
+        if constexpr (kSize == 4) out = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        else out = make_uint4(Element<TYPE>::narrow2(v[0], v[1]), Element<TYPE>::narrow2(v[2], v[3]),
+                              Element<TYPE>::narrow2(v[4], v[5]), Element<TYPE>::narrow2(v[6], v[7]));
+      }
+      if (m >= a.M || n >= a.N) continue;
+      uint8_t* to = TYPE == kSums ? reinterpret_cast<uint8_t*>(a.part) + (((uint64_t)blockIdx.y * a.M + m) * a.N + n) * 4
+                                  : reinterpret_cast<uint8_t*>(a.y) + (m * a.y_ld + n) * kSize;
+      if (a.wide && n + kPer <= a.N) {
+        *reinterpret_cast<uint4*>(to) = out;
+      } else {
+        const uint32_t w[4] = {out.x, out.y, out.z, out.w};
 #pragma unroll
         for (uint32_t e = 0; e < kPer; ++e) {
           if (n + e >= a.N) break;
-          if constexpr (kSize == 4) reinterpret_cast<uint32_t*>(out)[e] = w[e];
-          else reinterpret_cast<uint16_t*>(out)[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+          if constexpr (kSize == 4) reinterpret_cast<uint32_t*>(to)[e] = w[e];
+          else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
         }
       }
     }
-    wait_loads<63>();
-    __builtin_amdgcn_sched_barrier(0);
+    wait_loads<63>();   // (... and its reads)
   }
 }
 
-// The pieces' sums of one result, added in 64 bits.
-template <uint32_t TYPE>
-__global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
-  const uint64_t all = (uint64_t)a.M * a.N;
-  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
-    int64_t sum = 0;
-    for (uint32_t s = 0; s < a.splits; ++s) sum += a.part[s * all + i];
-    const uint32_t m = (uint32_t)(i / a.N), n = (uint32_t)(i % a.N);
-    put<TYPE>(a, m, n, scaled((float)sum, a.a_scale[m], a.b_scale[n]));
+// ---- few rows ---------------------------------------------------------------------
+// At most 32 rows of a: the weights' bytes are what it takes.  A workgroup has 16 NT of their rows and up to 16 wavefronts,
+// which take turns at 256 bytes of k; a lane loads 64 of them in a row (the order of k is the same for both
+// operands, so it need not be the matrix instruction's own), straight from memory: no two wavefronts share them.
+constexpr uint32_t kFewDepth = 256;
+
+template <int MT, int NT, uint32_t TYPE>
+__global__ __launch_bounds__(1024) void k_product_few(ProductArgs a) {
+  __shared__ __attribute__((aligned(16))) int sums[16][MT * NT * 256];
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const uint32_t n0 = blockIdx.x * 16 * NT, k0 = blockIdx.y * a.split_k, k1 = min(k0 + a.split_k, a.K);
+  const uint32_t own = 64 * (lane >> 4);
+  int4v acc[MT][NT] = {};
+  for (uint32_t k = k0 + wave * kFewDepth; k < k1; k += waves * kFewDepth) {
+    int4v w[NT][4], x[MT][4];
+    if (k + kFewDepth <= k1) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int8_t* p = a.b + (min(n0 + 16 * t + (lane & 15), a.N - 1) * a.b_ld + k + own);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[t][j] = reinterpret_cast<const int4v*>(p)[j];
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        const int8_t* p = a.a + (min(16 * t + (lane & 15), a.M - 1) * a.a_ld + k + own);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[t][j] = reinterpret_cast<const int4v*>(p)[j];
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[t][j] = operand(a.b, a.b_ld, n0 + 16 * t + (lane & 15), a.N, k + own + 16 * j, a.K);
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x[t][j] = masked(operand(a.a, a.a_ld, 16 * t + (lane & 15), a.M, k + own + 16 * j, a.K), k + own + 16 * j, a.K);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int u = 0; u < NT; ++u) acc[t][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][j], x[t][j], acc[t][u], 0, 0, 0);
   }
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+      *reinterpret_cast<int4v*>(&sums[wave][(16 * t + (lane & 15)) * (16 * NT) + 16 * u + 4 * (lane >> 4)]) = acc[t][u];
+  __syncthreads();
+  for (uint32_t o = threadIdx.x; o < MT * NT * 256; o += blockDim.x) {
+    const uint32_t m = o / (16 * NT), n = n0 + o % (16 * NT);
+    if (m >= a.M || n >= a.N) continue;
+    int sum = 0;
+    for (uint32_t s = 0; s < waves; ++s) sum += sums[s][o];
+    if constexpr (TYPE == kSums) a.part[((uint64_t)blockIdx.y * a.M + m) * a.N + n] = sum;
+    else put<TYPE>(a, m, n, (float)sum);
+  }
+}
+
+// The pieces' sums, added in 64 bits: PER neighbouring results of a row to a thread.
+template <uint32_t TYPE, int PER>
+__global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
+  const uint64_t all = (uint64_t)a.M * a.N, i = PER * ((uint64_t)blockIdx.x * 256 + threadIdx.x);
+  if (i >= all) return;
+  int64_t sum[PER] = {};
+  for (uint32_t s = 0; s < a.splits; ++s) {
+    int v[PER];
+    if constexpr (PER == 4) *reinterpret_cast<int4v*>(v) = *reinterpret_cast<const int4v*>(a.part + s * all + i);
+    else v[0] = a.part[s * all + i];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) sum[e] += v[e];
+  }
+  const uint32_t m = all >> 32 ? (uint32_t)(i / a.N) : (uint32_t)i / a.N, n = (uint32_t)(i - (uint64_t)m * a.N);
+#pragma unroll
+  for (int e = 0; e < PER; ++e) put<TYPE>(a, m, n + e, (float)sum[e]);
 }
 
 }  // namespace
 
+// Which kernel, and in how many pieces of k: the one that is expected to take the least time (us).  A tile kernel's
+// workgroups run in rounds of as many as the 256 compute units hold; a round takes a fixed time and one per stage of
+// 128 bytes of k, longer where several workgroups share a compute unit.  Few rows: the weights' bytes, a's rows that
+// every workgroup reads anew, and the turns of a wavefront.  Fitted to 62 products from 1 x 1024 x 1024 to 8192^3 that
+// every kernel was timed on: the choice takes at most 6% longer than the fastest on 58 of them, 24% on the worst
+// (us, the choice and the fastest: 2048 x 4096 x 1024 21.7 and 18.6; 1 x 16384 x 1024 6.2 and 5.0).
 ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
-  ProductPlan p = {1, kMostK, 0};
-  if (K > kMostK) {
-    p.splits = (K + kMostK - 1) / kMostK;
-    p.bytes = (uint64_t)p.splits * M * N * 4;
+  struct Kernel { uint32_t kind, size, slots; double fixed, alone, full; };
+  static constexpr Kernel kernels[] = {
+      {kProductTile64Deep, 64, 2, 2.3, 0.17, 0.37},
+      {kProductTile64, 64, 5, 1.9, 0.24, 1.2},
+      {kProductTile128, 128, 2, 3.2, 0.53, 0.97},
+      {kProductTile256, 256, 1, 12.0, 1.3, 1.3},
+  };
+  constexpr double kLaunch = 2.3, kCus = 256.0;
+  const uint32_t fewest = std::max(1u, (K + kMostK - 1) / kMostK);
+  auto join = [&](uint32_t splits) { return splits > 1 ? 3.8 + 8.0 * splits * M * N / 7.4e6 : 0.0; };
+  ProductPlan best = {};
+  double least = 1e300;
+  auto offer = [&](uint32_t kind, uint32_t splits, double us) {
+    if (us >= least) return;
+    least = us;
+    const uint32_t piece = splits == 1 ? kMostK : ((K + splits - 1) / splits + 255) / 256 * 256;
+    best = {kind, splits == 1 ? 1 : (K + piece - 1) / piece, piece, 0};
+  };
+  for (const Kernel& k : kernels) {
+    const double tiles = (double)((M + k.size - 1) / k.size) * ((N + k.size - 1) / k.size), slots = kCus * k.slots;
+    for (uint32_t splits = fewest; splits <= 16 * fewest; splits *= 2) {
+      if (splits > fewest && (K / splits < 1024 || tiles * splits > 2 * kCus)) break;
+      const double stages = std::ceil(K / 128.0 / splits), groups = tiles * splits;
+      auto round = [&](double n) {
+        const double share = k.slots == 1 ? 0.0 : std::max(0.0, std::ceil(n / kCus) - 1) / (k.slots - 1);
+        return k.fixed + stages * (k.alone + share * (k.full - k.alone));
+      };
+      const double rounds = std::floor(groups / slots), left = groups - rounds * slots;
+      offer(k.kind, splits, kLaunch + rounds * round(slots) + (left > 0 ? round(left) : 0.0) + join(splits));
+    }
   }
-  return p;
+  if (M <= 32)
+    offer(kProductFew, fewest, kLaunch + 1.4 + (double)N * K / 1.2e7 + (double)M * K * ((N + 15) / 16) / 1.4e7 + 1.3 * std::ceil(K / 4096.0) + join(fewest));
+  if (best.splits > 1) best.bytes = (uint64_t)best.splits * M * N * 4;
+  return best;
 }
 
 namespace {
-template <int MI, int NI>
-hipError_t launch_tiles(const ProductArgs& a, hipStream_t st) {
-  const dim3 grid((a.M + 64 * MI - 1) / (64 * MI) * ((a.N + 64 * NI - 1) / (64 * NI)), a.splits);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
-  if (a.part) go(k_product<MI, NI, kSums>);
-  else if (a.type == QSGD_TYPE_F32) go(k_product<MI, NI, QSGD_TYPE_F32>);
-  else if (a.type == QSGD_TYPE_BF16) go(k_product<MI, NI, QSGD_TYPE_BF16>);
-  else go(k_product<MI, NI, QSGD_TYPE_F16>);
-  return hipGetLastError();
+
+template <uint32_t TYPE>
+void launch_as(const ProductArgs& a, uint32_t kind, hipStream_t st) {
+  auto tiles = [&](auto kernel, uint32_t size) {
+    const dim3 grid((a.M + size - 1) / size * ((a.N + size - 1) / size), a.splits);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
+  };
+  if (kind == kProductFew) {
+    const uint32_t steps = (std::min(a.K, a.split_k) + kFewDepth - 1) / kFewDepth;
+    const dim3 block(64 * std::max(1u, std::min(steps, 16u)));
+    if (a.M <= 16) hipLaunchKernelGGL((k_product_few<1, 1, TYPE>), dim3((a.N + 15) / 16, a.splits), block, 0, st, a);
+    else hipLaunchKernelGGL((k_product_few<2, 1, TYPE>), dim3((a.N + 15) / 16, a.splits), block, 0, st, a);
+  }
+  else if (kind == kProductTile64Deep) tiles(k_product<1, 1, 4, TYPE>, 64);
+  else if (kind == kProductTile64) tiles(k_product<1, 1, 2, TYPE>, 64);
+  else if (kind == kProductTile128) tiles(k_product<2, 2, 2, TYPE>, 128);
+  else tiles(k_product<4, 4, 2, TYPE>, 256);
 }
+
 }  // namespace
 
-hipError_t launch_product(const ProductArgs& a, hipStream_t st) {
-  const uint64_t big = (uint64_t)((a.M + 255) / 256) * ((a.N + 255) / 256);
-  return big >= 128 ? launch_tiles<4, 4>(a, st) : launch_tiles<2, 2>(a, st);
+hipError_t launch_product(const ProductArgs& a, uint32_t kind, hipStream_t st) {
+  if (a.part) launch_as<kSums>(a, kind, st);
+  else if (a.type == QSGD_TYPE_F32) launch_as<QSGD_TYPE_F32>(a, kind, st);
+  else if (a.type == QSGD_TYPE_BF16) launch_as<QSGD_TYPE_BF16>(a, kind, st);
+  else launch_as<QSGD_TYPE_F16>(a, kind, st);
+  return hipGetLastError();
 }
 
 hipError_t launch_product_join(const ProductArgs& a, hipStream_t st) {
-  const uint64_t blocks = ((uint64_t)a.M * a.N + 255) / 256;
-  const dim3 grid((uint32_t)(blocks < 65536 ? blocks : 65536));
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
-  if (a.type == QSGD_TYPE_F32) go(k_product_join<QSGD_TYPE_F32>);
-  else if (a.type == QSGD_TYPE_BF16) go(k_product_join<QSGD_TYPE_BF16>);
-  else go(k_product_join<QSGD_TYPE_F16>);
+  const uint64_t all = (uint64_t)a.M * a.N;
+  auto go = [&](auto four, auto one) {
+    if (a.N % 4 == 0) hipLaunchKernelGGL(four, dim3((uint32_t)((all / 4 + 255) / 256)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(one, dim3((uint32_t)((all + 255) / 256)), dim3(256), 0, st, a);
+  };
+  if (a.type == QSGD_TYPE_F32) go(k_product_join<QSGD_TYPE_F32, 4>, k_product_join<QSGD_TYPE_F32, 1>);
+  else if (a.type == QSGD_TYPE_BF16) go(k_product_join<QSGD_TYPE_BF16, 4>, k_product_join<QSGD_TYPE_BF16, 1>);
+  else go(k_product_join<QSGD_TYPE_F16, 4>, k_product_join<QSGD_TYPE_F16, 1>);
   return hipGetLastError();
 }
 
