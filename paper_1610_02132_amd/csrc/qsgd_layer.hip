@@ -89,49 +89,50 @@ int dropout(const qsgd_draws* draws, float p, const qsgd_matrix* x, const qsgd_m
 
 // Workspace of a column form.
 struct ColumnSpace {
-  uint32_t chunks, chunk_rows;
-  uint64_t max_at, sum_at, inv_at, bytes;
+  uint32_t strip_lanes, chunks, chunk_rows;
+  uint64_t max_at, sum_at, bytes;
 };
 ColumnSpace column_space(uint64_t rows, uint64_t cols) {
   ColumnSpace s = {};
-  plan_columns((uint32_t)rows, (uint32_t)cols, s.chunks, s.chunk_rows);
-  const uint64_t each = padded(4 * cols * s.chunks);
-  s.max_at = 0;
-  s.sum_at = each;
-  s.inv_at = 2 * each;
-  s.bytes = 2 * each + padded(4 * cols);
+  plan_columns((uint32_t)rows, (uint32_t)cols, s.strip_lanes, s.chunks, s.chunk_rows);
+  s.sum_at = padded(4 * cols * s.chunks);
+  s.bytes = 2 * s.sum_at;
   return s;
 }
 
-void fill(QuantizeArgs& q, const qsgd_matrix* x, const DrawArgs& draws, bool stochastic) {
+QuantizeArgs job(const qsgd_matrix* x, const DrawArgs& draws) {
+  QuantizeArgs q = {};
   q.x = x->data_dev; q.ld = x->ld;
   q.rows = (uint32_t)x->rows; q.cols = (uint32_t)x->cols;
   q.wide = wide(x);
-  q.stochastic = stochastic;
   q.draws = draws;
+  return q;
 }
-// scale: or null, where only the sums are wanted (levels without rows have no address either)
-void fill_columns(QuantizeArgs& q, const ColumnSpace& s, uint8_t* ws, int8_t* levels, uint64_t ld, float* scale, float* sum) {
+void want_rows(QuantizeArgs& q, int8_t* levels, uint64_t ld, float* scale) {
+  q.q_rows = levels; q.q_rows_ld = ld; q.row_scale = scale;
+}
+// scale: or null, where only the sums are wanted
+void want_columns(QuantizeArgs& q, uint8_t* ws, int8_t* levels, uint64_t ld, float* scale, float* sum) {
+  const ColumnSpace s = column_space(q.rows, q.cols);
   q.q_cols = levels; q.q_cols_ld = ld; q.col_scale = scale;
-  q.chunks = s.chunks; q.chunk_rows = s.chunk_rows;
-  q.part_max = scale ? reinterpret_cast<uint32_t*>(ws + s.max_at) : nullptr;
-  q.part_sum = sum ? reinterpret_cast<float*>(ws + s.sum_at) : nullptr;
-  q.col_max = reinterpret_cast<float*>(ws + s.inv_at);
+  q.strip_lanes = s.strip_lanes; q.chunks = s.chunks; q.chunk_rows = s.chunk_rows;
+  // (without rows there is no workspace either, and nothing is read there)
+  q.part_max = scale ? reinterpret_cast<uint32_t*>(s.bytes ? ws + s.max_at : reinterpret_cast<uint8_t*>(scale)) : nullptr;
+  q.part_sum = sum ? reinterpret_cast<float*>(s.bytes ? ws + s.sum_at : reinterpret_cast<uint8_t*>(sum)) : nullptr;
   q.col_sum = sum;
 }
 
-int quantize_rows(const QuantizeArgs& q, uint32_t type, hipStream_t st) {
-  ScopedTiming tm("quantize_rows", st);
-  return status(launch_quantize_rows(q, type, st));
-}
-int quantize_columns(const QuantizeArgs& q, uint32_t type, hipStream_t st) {
+int quantize(QuantizeJobs& jobs, uint32_t type, uint32_t rounding, hipStream_t st) {
+  const bool stochastic = rounding == QSGD_ROUND_STOCHASTIC;
   {
-    ScopedTiming tm("column_max", st);
-    if (int rc = status(launch_column_max(q, type, st))) return rc;
+    ScopedTiming tm("quantize_rows", st);
+    if (int rc = status(launch_quantize(jobs, type, stochastic, st, false))) return rc;
   }
-  if (!q.col_scale || !q.rows) return QSGD_OK;
+  bool columns = false;
+  for (uint32_t j = 0; j < jobs.count; ++j) columns |= jobs.job[j].part_max || jobs.job[j].part_sum;
+  if (!columns) return QSGD_OK;
   ScopedTiming tm("quantize_columns", st);
-  return status(launch_quantize_columns(q, type, st));
+  return status(launch_quantize(jobs, type, stochastic, st, true));
 }
 
 // ---- product ---------------------------------------------------------------------
@@ -170,10 +171,11 @@ bool room(const void* ws, size_t have, uint64_t need) { return need == 0 || (ws 
 // Why a workspace is refused.
 int no_room(const void* ws, uint64_t need) { return need && (!ws || !aligned(ws, 16)) ? QSGD_ERR_INVALID_ARG : QSGD_ERR_CAPACITY; }
 
-// Workspace of the layer's gradients: levels and scales of its operands, then what their making and the products need,
-// one after the other.
+// Workspace of the layer's gradients: levels and scales of its operands, the columns' maxima and sums, and what the
+// products need, one after the other.
 struct BackwardSpace {
-  uint64_t dy_rows, dy_row_scale, w_cols, w_scale, dy_cols, dy_col_scale, x_cols, x_scale, rest, bytes;
+  uint64_t dy_rows, dy_row_scale, w_cols, w_scale, dy_cols, dy_col_scale, x_cols, x_scale;
+  uint64_t dy_space, w_space, x_space, rest, bytes;
 };
 BackwardSpace backward_space(uint64_t M, uint64_t N, uint64_t K) {
   BackwardSpace s = {};
@@ -183,10 +185,11 @@ BackwardSpace backward_space(uint64_t M, uint64_t N, uint64_t K) {
   s.w_cols = take(K * levels_ld(N)); s.w_scale = take(4 * K);
   s.dy_cols = take(N * levels_ld(M)); s.dy_col_scale = take(4 * N);
   s.x_cols = take(K * levels_ld(M)); s.x_scale = take(4 * K);
-  s.rest = at;
-  uint64_t rest = std::max(product_bytes(M, K, N), product_bytes(N, K, M));
-  for (const auto& [r, c] : {std::pair{M, N}, std::pair{N, K}, std::pair{M, K}}) rest = std::max(rest, column_space(r, c).bytes);
-  s.bytes = at + padded(rest);
+  s.dy_space = take(column_space(M, N).bytes);
+  s.w_space = take(column_space(N, K).bytes);
+  s.x_space = take(column_space(M, K).bytes);
+  s.rest = take(std::max(product_bytes(M, K, N), product_bytes(N, K, M)));
+  s.bytes = at;
   return s;
 }
 
@@ -216,25 +219,17 @@ int qsgd_quantize(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix*
   if (columns && (!sound(columns, true) || !shaped(columns, x->cols, x->rows) || !floats(column_scale_dev, x->cols) ||
                   overlap(x, columns) || (rows && overlap(rows, columns))))
     return QSGD_ERR_INVALID_ARG;
-  QuantizeArgs q = {};
   DrawArgs d = {};
   if (rounding == QSGD_ROUND_STOCHASTIC || draws)
     if (int rc = draw_args(draws, x->rows, d)) return rc;
   const uint64_t need = columns ? qsgd_quantize_workspace_bytes(x->rows, x->cols) : 0;
   if (!room(workspace_dev, workspace_bytes, need)) return no_room(workspace_dev, need);
-  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-  fill(q, x, d, rounding == QSGD_ROUND_STOCHASTIC);
-  if (rows && x->rows) {
-    q.q_rows = reinterpret_cast<int8_t*>(rows->data_dev); q.q_rows_ld = rows->ld; q.row_scale = row_scale_dev;
-    if (int rc = quantize_rows(q, x->type, st)) return rc;
-  }
-  if (columns && x->cols) {
-    const ColumnSpace s = column_space(x->rows, x->cols);
-    fill_columns(q, s, reinterpret_cast<uint8_t*>(workspace_dev), reinterpret_cast<int8_t*>(columns->data_dev), columns->ld,
-                 column_scale_dev, nullptr);
-    if (int rc = quantize_columns(q, x->type, st)) return rc;
-  }
-  return QSGD_OK;
+  QuantizeJobs jobs = {1, {job(x, d)}};
+  if (rows && x->rows) want_rows(jobs.job[0], reinterpret_cast<int8_t*>(rows->data_dev), rows->ld, row_scale_dev);
+  if (columns && x->cols)
+    want_columns(jobs.job[0], reinterpret_cast<uint8_t*>(workspace_dev), reinterpret_cast<int8_t*>(columns->data_dev),
+                 columns->ld, column_scale_dev, nullptr);
+  return quantize(jobs, x->type, rounding, reinterpret_cast<hipStream_t>(hip_stream));
 }
 
 size_t qsgd_int_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
@@ -273,7 +268,6 @@ int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_m
       overlap(x, y) || overlap(w, y))
     return QSGD_ERR_INVALID_ARG;
   if (w->ld >= kMostLd || levels_ld(x->cols) >= kMostLd || too_many(y->rows, y->cols)) return QSGD_ERR_UNSUPPORTED;
-  QuantizeArgs q = {};
   DrawArgs d = {};
   if (rounding == QSGD_ROUND_STOCHASTIC || draws)
     if (int rc = draw_args(draws, x->rows, d)) return rc;
@@ -283,9 +277,10 @@ int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_m
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   uint8_t* ws = reinterpret_cast<uint8_t*>(workspace_dev);
   const uint64_t ld = levels_ld(x->cols), scale_at = padded(x->rows * ld), rest = scale_at + padded(4 * x->rows);
-  fill(q, x, d, rounding == QSGD_ROUND_STOCHASTIC);
-  q.q_rows = reinterpret_cast<int8_t*>(ws); q.q_rows_ld = ld; q.row_scale = reinterpret_cast<float*>(ws + scale_at);
-  if (int rc = quantize_rows(q, x->type, st)) return rc;
+  QuantizeJobs jobs = {1, {job(x, d)}};
+  QuantizeArgs& q = jobs.job[0];
+  want_rows(q, reinterpret_cast<int8_t*>(ws), ld, reinterpret_cast<float*>(ws + scale_at));
+  if (int rc = quantize(jobs, x->type, rounding, st)) return rc;
   ProductArgs p = {};
   p.a = q.q_rows; p.a_ld = ld;
   p.b = reinterpret_cast<const int8_t*>(w->data_dev); p.b_ld = w->ld;
@@ -316,7 +311,6 @@ int qsgd_linear_backward(const qsgd_draws* draws, uint32_t rounding, const qsgd_
   if (dx && dw && overlap(dx, dw)) return QSGD_ERR_INVALID_ARG;
   const uint64_t M = x->rows, N = w->rows, K = x->cols;
   if (levels_ld(N) >= kMostLd || levels_ld(M) >= kMostLd || too_many(M, K) || too_many(N, K)) return QSGD_ERR_UNSUPPORTED;
-  QuantizeArgs base = {};
   DrawArgs d = {};
   if (rounding == QSGD_ROUND_STOCHASTIC || draws) {
     if (int rc = draw_args(draws, M, d)) return rc;
@@ -330,19 +324,25 @@ int qsgd_linear_backward(const qsgd_draws* draws, uint32_t rounding, const qsgd_
   DrawArgs draws_w = d, draws_x = d;
   draws_w.stream_id += 1; draws_w.row_base = 0;
   draws_x.stream_id += 2;
-  const bool stochastic = rounding == QSGD_ROUND_STOCHASTIC;
-  const bool want_dx = dx && M && K, want_dw = dw && N && K;
-  if ((want_dw || db_dev) && N) {   // dy by columns, and its sums
-    fill(base, dy, d, stochastic);
-    fill_columns(base, column_space(M, N), ws + s.rest, levels(s.dy_cols), levels_ld(M),
-                 want_dw ? scales(s.dy_col_scale) : nullptr, db_dev);
-    if (int rc = quantize_columns(base, dy->type, st)) return rc;
+  const bool want_dx = dx && M && K, want_dw = dw && N && K, want_db = db_dev && N;
+  QuantizeJobs jobs = {};
+  {
+    QuantizeArgs& q = jobs.job[jobs.count++] = job(dy, d);
+    if (want_dx) want_rows(q, levels(s.dy_rows), levels_ld(N), scales(s.dy_row_scale));
+    if (want_dw || want_db)
+      want_columns(q, ws + s.dy_space, levels(s.dy_cols), levels_ld(M), want_dw ? scales(s.dy_col_scale) : nullptr,
+                   want_db ? db_dev : nullptr);
+  }
+  if (want_dx) {
+    QuantizeArgs& q = jobs.job[jobs.count++] = job(w, draws_w);
+    want_columns(q, ws + s.w_space, levels(s.w_cols), levels_ld(N), scales(s.w_scale), nullptr);
   }
   if (want_dw) {
-    QuantizeArgs q = {};
-    fill(q, x, draws_x, stochastic);
-    fill_columns(q, column_space(M, K), ws + s.rest, levels(s.x_cols), levels_ld(M), scales(s.x_scale), nullptr);
-    if (int rc = quantize_columns(q, x->type, st)) return rc;
+    QuantizeArgs& q = jobs.job[jobs.count++] = job(x, draws_x);
+    want_columns(q, ws + s.x_space, levels(s.x_cols), levels_ld(M), scales(s.x_scale), nullptr);
+  }
+  if (int rc = quantize(jobs, x->type, rounding, st)) return rc;
+  if (want_dw) {
     ProductArgs p = {};
     p.a = levels(s.dy_cols); p.b = levels(s.x_cols); p.a_ld = p.b_ld = levels_ld(M);
     p.M = (uint32_t)N; p.N = (uint32_t)K; p.K = (uint32_t)M;
@@ -351,13 +351,6 @@ int qsgd_linear_backward(const qsgd_draws* draws, uint32_t rounding, const qsgd_
     if (int rc = product(p, ws + s.rest, st)) return rc;
   }
   if (want_dx) {
-    QuantizeArgs r = {}, q = {};
-    fill(r, dy, d, stochastic);
-    r.q_rows = levels(s.dy_rows); r.q_rows_ld = levels_ld(N); r.row_scale = scales(s.dy_row_scale);
-    if (int rc = quantize_rows(r, dy->type, st)) return rc;
-    fill(q, w, draws_w, stochastic);
-    fill_columns(q, column_space(N, K), ws + s.rest, levels(s.w_cols), levels_ld(N), scales(s.w_scale), nullptr);
-    if (int rc = quantize_columns(q, w->type, st)) return rc;
     ProductArgs p = {};
     p.a = levels(s.dy_rows); p.b = levels(s.w_cols); p.a_ld = p.b_ld = levels_ld(N);
     p.M = (uint32_t)M; p.N = (uint32_t)K; p.K = (uint32_t)N;

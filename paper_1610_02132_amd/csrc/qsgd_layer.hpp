@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "qsgd.h"
 #include "qsgd_device.hpp"
 
@@ -120,29 +122,29 @@ hipError_t launch_dropout(const DropoutArgs& a, uint32_t type, hipStream_t st);
 
 // ---- quantizer ---------------------------------------------------------------------
 constexpr float kTinyMax = 0x1p-119f;   // rows whose largest magnitude is below it count as zero: 127 / m and m / 127 stay normal
-constexpr uint32_t kStripCols = 512;    // columns that a workgroup of the column maxima covers
+constexpr uint32_t kTileRows = 512;     // rows that a workgroup of the column form takes
 
 struct QuantizeArgs {
   const void* x;
   uint64_t ld;
   uint32_t rows, cols;
   bool wide;                  // every row of x is aligned to 16 bytes
-  bool stochastic;
   DrawArgs draws;
-  int8_t* q_rows; uint64_t q_rows_ld; float* row_scale;   // or null
-  int8_t* q_cols; uint64_t q_cols_ld; float* col_scale;   // or null
+  int8_t* q_rows; uint64_t q_rows_ld; float* row_scale;   // row_scale: or null
+  int8_t* q_cols; uint64_t q_cols_ld; float* col_scale;
   // workspace of the column form
-  uint32_t chunks, chunk_rows;
-  uint32_t* part_max;         // chunks x cols: largest magnitude's bits as fp32
+  uint32_t strip_lanes, chunks, chunk_rows;
+  uint32_t* part_max;         // chunks x cols: largest magnitude's bits as fp32; or null: no column form
   float* part_sum;            // chunks x cols, or null: sums of the columns
-  float* col_max;             // cols
-  float* col_sum;             // or null: the sums' destination
+  float* col_sum;             // where the sums go
+  // workgroups (launch_quantize)
+  uint32_t row_lanes, row_blocks, max_blocks, tile_blocks;
 };
-// Rows of a chunk and how many there are.
-void plan_columns(uint32_t rows, uint32_t cols, uint32_t& chunks, uint32_t& chunk_rows);
-hipError_t launch_quantize_rows(const QuantizeArgs& a, uint32_t type, hipStream_t st);
-hipError_t launch_column_max(const QuantizeArgs& a, uint32_t type, hipStream_t st);
-hipError_t launch_quantize_columns(const QuantizeArgs& a, uint32_t type, hipStream_t st);
+struct QuantizeJobs { uint32_t count; QuantizeArgs job[3]; };
+// Lanes to a row of a strip of columns, rows of a chunk, and how many chunks there are.
+void plan_columns(uint32_t rows, uint32_t cols, uint32_t& strip_lanes, uint32_t& chunks, uint32_t& chunk_rows);
+// First launch: row forms, and the columns' maxima and sums; second: column forms.
+hipError_t launch_quantize(QuantizeJobs& jobs, uint32_t type, bool stochastic, hipStream_t st, bool second);
 
 // ---- product -----------------------------------------------------------------------
 struct ProductArgs {

@@ -1,67 +1,137 @@
 // Quantizer Q_s of Sec. 3.1 (Eq. 2) with s = 127 and max scaling (Sec. 4), a bucket being a row or a
-// column of a matrix, levels as signed bytes.  Memory bound: the row form reads a row once more than
-// it has to (from the cache), the column form reads the matrix twice (maxima, then levels, which leave
-// transposed through LDS).
+// column of a matrix, levels as signed bytes.  Two launches for any number of matrices: the first makes the row forms and the
+// columns' largest magnitudes (and sums) over chunks of rows, the second the column forms, transposed through LDS.
+// Memory bound: the row form reads a row once, the column form reads the matrix twice (a column does not fit
+// a compute unit).
 #include "qsgd_layer.hpp"
 
 namespace qsgd {
 namespace {
 
 // Largest magnitude -> scale and the factor fl(127 / m); zero rows get zeros, rows with an infinity or a NaN
-// the scale NaN and levels 0.
+// the scale NaN and the factor 0.
 __device__ __forceinline__ void scale_of(float m, float& scale, float& inv) {
   const bool finite = m < __builtin_huge_valf(), tiny = m < kTinyMax;
   inv = finite && !tiny ? 127.0f / m : 0.0f;
   scale = !finite ? __builtin_nanf("") : tiny ? 0.0f : m / 127.0f;
 }
 
-// The level of one value as a signed byte.
-__device__ __forceinline__ uint32_t level_of(float v, float inv, bool stochastic, uint32_t h) {
-  // a row that holds an infinity or a NaN has inv = 0 and products that are NaN, else |t| <= 127 (1 + 2^-23)
-  const float t = inv > 0.0f ? v * inv : 0.0f;
-  int level;
-  if (stochastic) {
-    const float a = fabsf(t), low = floorf(a), u = ((float)h + 0.5f) * 0x1p-16f;
-    level = min((int)low + (u < a - low ? 1 : 0), 127);
-    level = t < 0.0f ? -level : level;
-  } else {
-    level = (int)rintf(t);
-  }
-  return (uint32_t)level & 0xFFu;
+// Four words' bytes of one number in a word.
+template <int BYTE>
+__device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0C0C0400u | BYTE << 8 | BYTE);
+  const uint32_t hi = __builtin_amdgcn_perm(d, c, 0x04000C0Cu | (uint32_t)BYTE << 24 | (uint32_t)BYTE << 16);
+  return lo | hi;
 }
 
-// The larger of two magnitudes by their bits: a NaN's are above infinity's.
-__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+// The levels of four values t (scaled to 127) as signed bytes of a word.  An infinity or a NaN in t (inv is 0 then, or the
+// value itself) becomes level 0: the conversions to whole numbers say 0 for a NaN, and 0 times an infinity is one.
+__device__ __forceinline__ uint32_t nearest_levels(const float (&t)[4]) {
+  int q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = (int)__builtin_rintf(t[i]);
+  return pack_bytes<0>(q[0], q[1], q[2], q[3]);
+}
 
-template <uint32_t TYPE>
-__global__ __launch_bounds__(256) void k_quantize_rows(QuantizeArgs a) {
-  const uint32_t r = blockIdx.x, c8s = (a.cols + 7) / 8, iteration = draw_iteration(a.draws);
-  __shared__ uint32_t part[4];
-  uint32_t m = 0;
-  for (uint32_t c8 = threadIdx.x; c8 < c8s; c8 += 256) {
+// Up iff (h + 1/2) / 65536 is below the fraction of |t|:  with R = ceil(65536 |t| - 1/2), a whole number that fp32
+// holds exactly (|t| <= 127 + 2^-17, the next number after 127, so that R <= 127 * 65536 and no level passes 127),
+// the level is the upper half of R + 65535 - h.  `left` has 65535 - h.
+__device__ __forceinline__ uint32_t stochastic_levels(const float (&t)[4], const uint32_t (&left)[4]) {
+  uint32_t q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    q[i] = (uint32_t)__builtin_ceilf(__builtin_fmaf(fabsf(t[i]), 65536.0f, -0.5f)) + left[i];
+  const uint32_t level = pack_bytes<2>(q[0], q[1], q[2], q[3]);
+  // a byte of ones where t is negative, and the negative of those bytes: no carry leaves bit 7, which is put in last
+  const uint32_t minus = __builtin_amdgcn_perm(__float_as_uint(t[1]), __float_as_uint(t[0]), 0x0C0C0B09u) |
+                         __builtin_amdgcn_perm(__float_as_uint(t[3]), __float_as_uint(t[2]), 0x0B090C0Cu);
+  const uint32_t flipped = level ^ minus;
+  return ((flipped & 0x7F7F7F7Fu) + (minus & 0x01010101u)) ^ (flipped & 0x80808080u);
+}
+
+// 65535 - h for the draws of column i of a block.
+__device__ __forceinline__ uint32_t draw_left(const HalfWords& h, int i) { return 0xFFFFu - half_word(h, i); }
+
+// Magnitudes' bits, whose order is that of the magnitudes with a NaN above infinity: eight columns, two to a word for
+// 16-bit types.
+template <uint32_t TYPE> struct Largest {
+  static constexpr int kWords = Eight<TYPE>::kWords;
+  uint32_t w[kWords] = {};
+  __device__ __forceinline__ void add(const Eight<TYPE>& x) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (kWords == 8) {
+        w[i] = max(w[i], x.w[i] & 0x7FFFFFFFu);
+      } else {
+        using pair = __attribute__((ext_vector_type(2))) uint16_t;
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(pair, w[i]),
+                                                                      __builtin_bit_cast(pair, x.w[i] & 0x7FFF7FFFu)));
+      }
+    }
+  }
+  // ... as bits of fp32
+  __device__ __forceinline__ uint32_t column(int i) const {
+    Eight<TYPE> e;
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) e.w[j] = w[j];
+    return __float_as_uint(e.value(i));
+  }
+};
+
+constexpr int kHeld = 4;   // blocks of eight columns of a row that a lane holds in registers
+
+// Rows `first` and following, one to 256 / LANES of the workgroup's parts.
+template <uint32_t TYPE, bool STOCHASTIC, int LANES>
+__device__ __forceinline__ void rows_block(const QuantizeArgs& a, uint32_t first, uint32_t* shared) {
+  const uint32_t lane = threadIdx.x % LANES, r = first + threadIdx.x / LANES, c8s = (a.cols + 7) / 8;
+  const bool have = r < a.rows;
+  Eight<TYPE> held[kHeld];
+  Largest<TYPE> most;
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    const uint32_t c8 = u * LANES + lane;
+    if (have && c8 < c8s) {
+      held[u].load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8, a.wide);
+      most.add(held[u]);
+    }
+  }
+  for (uint32_t c8 = kHeld * LANES + lane; have && c8 < c8s; c8 += LANES) {
     Eight<TYPE> x;
     x.load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8, a.wide);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, magnitude(x.value(i)));
+    most.add(x);
   }
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, most.column(i));
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
-  __syncthreads();
-  m = max(max(part[0], part[1]), max(part[2], part[3]));
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = max(max(shared[0], shared[1]), max(shared[2], shared[3]));
+  }
+  if (!have) return;
   float scale, inv;
   scale_of(__uint_as_float(m), scale, inv);
-  if (threadIdx.x == 0) a.row_scale[r] = scale;
-  for (uint32_t c8 = threadIdx.x; c8 < c8s; c8 += 256) {
-    Eight<TYPE> x;
-    const uint32_t n = a.cols - 8 * c8;
-    x.load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), n, a.wide);
+  if (lane == 0) a.row_scale[r] = scale;
+  const uint32_t iteration = STOCHASTIC ? draw_iteration(a.draws) : 0;
+  auto put = [&](const Eight<TYPE>& x, uint32_t c8) {
     HalfWords h = {};
-    if (a.stochastic) h = draw_block(a.draws, iteration, r, c8);
-    uint32_t q[2] = {0, 0};
+    if constexpr (STOCHASTIC) h = draw_block(a.draws, iteration, r, c8);
+    uint32_t q[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i >> 2] |= level_of(x.value(i), inv, a.stochastic, half_word(h, i)) << (8 * (i & 3));
+    for (int half = 0; half < 2; ++half) {
+      float t[4];
+      uint32_t left[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        t[i] = x.value(4 * half + i) * inv;
+        left[i] = draw_left(h, 4 * half + i);
+      }
+      q[half] = STOCHASTIC ? stochastic_levels(t, left) : nearest_levels(t);
+    }
     int8_t* out = a.q_rows + (r * a.q_rows_ld + 8 * c8);
+    const uint32_t n = a.cols - 8 * c8;
     if (n >= 8) {
       *reinterpret_cast<uint2*>(out) = make_uint2(q[0], q[1]);
     } else {
@@ -69,140 +139,240 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantizeArgs a) {
       for (int i = 0; i < 7; ++i)
         if ((uint32_t)i < n) out[i] = (int8_t)(q[i >> 2] >> (8 * (i & 3)));
     }
+  };
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    const uint32_t c8 = u * LANES + lane;
+    if (c8 < c8s) put(held[u], c8);
+  }
+  for (uint32_t c8 = kHeld * LANES + lane; c8 < c8s; c8 += LANES) {
+    Eight<TYPE> x;
+    x.load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8, a.wide);
+    put(x, c8);
   }
 }
 
-// Maxima (and sums) of a strip of 512 columns over a chunk of rows: a wavefront reads a row of the strip
-// at a time.
+// Maxima (and sums) of 8 * a.strip_lanes columns over a chunk of rows; strip_lanes lanes read a row of them.
 template <uint32_t TYPE>
-__global__ __launch_bounds__(256) void k_column_max(QuantizeArgs a) {
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t c = blockIdx.x * kStripCols + 8 * lane;
-  const uint32_t r0 = blockIdx.y * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
-  __shared__ uint32_t maxima[4][kStripCols];
-  __shared__ float sums[4][kStripCols];
-  uint32_t m[8] = {};
+__device__ __forceinline__ void columns_block(const QuantizeArgs& a, uint32_t block, uint32_t* shared) {
+  const uint32_t lanes = a.strip_lanes, strips = (a.cols + 8 * lanes - 1) / (8 * lanes);
+  const uint32_t lane = threadIdx.x % lanes, part = threadIdx.x / lanes, parts = 256 / lanes;
+  const uint32_t strip = block % strips, chunk = block / strips, c = 8 * (strip * lanes + lane);
+  const uint32_t r0 = chunk * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
+  Largest<TYPE> most;
   float s[8] = {};
+  const bool sums = a.part_sum != nullptr;
   if (c < a.cols) {
-    for (uint32_t r = r0 + wave; r < r1; r += 4) {
+    auto take = [&](const Eight<TYPE>& x) {
+      most.add(x);
+      if (sums) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += x.value(i);
+      }
+    };
+    uint32_t r = r0 + part;
+    for (; r + 3 * parts < r1; r += 4 * parts) {   // (four rows on their way)
+      Eight<TYPE> x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u].load(element_at<TYPE>(a.x, a.ld, r + u * parts, c), a.cols - c, a.wide);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) take(x[u]);
+    }
+    for (; r < r1; r += parts) {
       Eight<TYPE> x;
       x.load(element_at<TYPE>(a.x, a.ld, r, c), a.cols - c, a.wide);
+      take(x);
+    }
+  }
+  // the parts' results, joined by halves
+  float* const sum = reinterpret_cast<float*>(shared + 256 * 8);
+  auto at = [&](uint32_t t, int i) { return 256 * i + t; };
+  uint32_t m[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    m[i] = most.column(i);
+    shared[at(threadIdx.x, i)] = m[i];
+    if (sums) sum[at(threadIdx.x, i)] = s[i];
+  }
+  for (uint32_t half = 128; half >= lanes; half >>= 1) {
+    __syncthreads();
+    if (threadIdx.x < half) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        m[i] = max(m[i], magnitude(x.value(i)));
-        s[i] += x.value(i);
+        m[i] = max(m[i], shared[at(threadIdx.x + half, i)]);
+        shared[at(threadIdx.x, i)] = m[i];
+        if (sums) {
+          s[i] += sum[at(threadIdx.x + half, i)];
+          sum[at(threadIdx.x, i)] = s[i];
+        }
       }
     }
   }
+  if (threadIdx.x < lanes) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { maxima[wave][8 * lane + i] = m[i]; sums[wave][8 * lane + i] = s[i]; }
-  __syncthreads();
-  for (uint32_t j = threadIdx.x; j < kStripCols; j += 256) {
-    const uint32_t col = blockIdx.x * kStripCols + j;
-    if (col >= a.cols) continue;
-    const uint64_t at = (uint64_t)blockIdx.y * a.cols + col;
-    if (a.part_max) a.part_max[at] = max(max(maxima[0][j], maxima[1][j]), max(maxima[2][j], maxima[3][j]));
-    if (a.part_sum) a.part_sum[at] = (sums[0][j] + sums[1][j]) + (sums[2][j] + sums[3][j]);
-  }
-}
-
-// One column per thread: the chunks' maxima and sums.
-__global__ __launch_bounds__(256) void k_column_scale(QuantizeArgs a) {
-  const uint32_t c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= a.cols) return;
-  uint32_t m = 0;
-  float s = 0.0f;
-  for (uint32_t k = 0; k < a.chunks; ++k) {
-    if (a.part_max) m = max(m, a.part_max[(uint64_t)k * a.cols + c]);
-    if (a.part_sum) s += a.part_sum[(uint64_t)k * a.cols + c];
-  }
-  if (a.part_max) {
-    float scale, inv;
-    scale_of(__uint_as_float(m), scale, inv);
-    a.col_max[c] = inv;
-    a.col_scale[c] = scale;
-  }
-  if (a.part_sum) a.col_sum[c] = s;
-}
-
-// A tile of 128 rows and 64 columns: a thread quantizes 8 columns of 4 rows, whose levels of one column make
-// a word in LDS; the tile leaves as 64 rows of 128 bytes.
-constexpr uint32_t kTileRows = 128, kTileCols = 64;
-
-template <uint32_t TYPE>
-__global__ __launch_bounds__(256) void k_quantize_columns(QuantizeArgs a) {
-  __shared__ uint32_t tile[kTileCols][kTileRows / 4 + 1];
-  const uint32_t strips = (a.cols + kTileCols - 1) / kTileCols;
-  const uint32_t c0 = blockIdx.x % strips * kTileCols, r0 = blockIdx.x / strips * kTileRows;
-  const uint32_t c = c0 + 8 * (threadIdx.x & 7), r = r0 + 4 * (threadIdx.x >> 3);
-  const uint32_t iteration = draw_iteration(a.draws);
-  if (c < a.cols) {
-    float inv[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) inv[i] = c + i < a.cols ? a.col_max[c + i] : 0.0f;
-    uint32_t q[8] = {};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (r + j >= a.rows) break;
-      Eight<TYPE> x;
-      x.load(element_at<TYPE>(a.x, a.ld, r + j, c), a.cols - c, a.wide);
-      HalfWords h = {};
-      if (a.stochastic) h = draw_block(a.draws, iteration, r + j, c / 8);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) q[i] |= level_of(x.value(i), inv[i], a.stochastic, half_word(h, i)) << (8 * j);
+    for (int i = 0; i < 8; ++i) {
+      if (c + i >= a.cols) break;
+      const uint64_t to = (uint64_t)chunk * a.cols + c + i;
+      if (a.part_max) a.part_max[to] = m[i];
+      if (sums) a.part_sum[to] = s[i];
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) tile[8 * (threadIdx.x & 7) + i][threadIdx.x >> 3] = q[i];
   }
-  __syncthreads();
-  for (uint32_t j = threadIdx.x; j < kTileCols * (kTileRows / 4); j += 256) {
-    const uint32_t col = j / (kTileRows / 4), w = j % (kTileRows / 4), row = r0 + 4 * w;
-    if (c0 + col >= a.cols || row >= a.rows) continue;
-    int8_t* out = a.q_cols + ((c0 + col) * a.q_cols_ld + row);
-    const uint32_t v = tile[col][w], n = a.rows - row;
-    if (n >= 4) *reinterpret_cast<uint32_t*>(out) = v;
-    else for (uint32_t i = 0; i < n; ++i) out[i] = (int8_t)(v >> (8 * i));
+}
+
+template <uint32_t TYPE, bool STOCHASTIC>
+__global__ __launch_bounds__(256) void k_quantize_rows(QuantizeJobs jobs) {
+  __shared__ uint32_t shared[2 * 256 * 8];
+  uint32_t block = blockIdx.x;
+  for (uint32_t j = 0; j < jobs.count; ++j) {
+    const QuantizeArgs& a = jobs.job[j];
+    if (block < a.row_blocks) {
+      if (a.row_lanes == 64) rows_block<TYPE, STOCHASTIC, 64>(a, 4 * block, shared);
+      else rows_block<TYPE, STOCHASTIC, 256>(a, block, shared);
+      return;
+    }
+    block -= a.row_blocks;
+    if (block < a.max_blocks) return columns_block<TYPE>(a, block, shared);
+    block -= a.max_blocks;
+  }
+}
+
+// The column form of 64 columns and up to 512 rows, 128 rows at a time: a thread quantizes 8 columns of 4 rows, whose
+// levels of one column make a word in LDS; 16 bytes of a column's 128 leave with a lane.
+template <uint32_t TYPE, bool STOCHASTIC>
+__global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
+  __shared__ __attribute__((aligned(16))) uint32_t tile[64 * 32];
+  __shared__ uint32_t found[4][64];
+  __shared__ float added[4][64], factor[64];
+  uint32_t block = blockIdx.x, j = 0;
+  while (block >= jobs.job[j].tile_blocks) block -= jobs.job[j++].tile_blocks;   // (the grid is their sum)
+  const QuantizeArgs& a = jobs.job[j];
+  const uint32_t strips = (a.cols + 63) / 64, c0 = block % strips * 64, first = block / strips * kTileRows;
+  {   // the chunks' maxima and sums, by four threads to a column
+    const uint32_t c = c0 + (threadIdx.x & 63), part = threadIdx.x >> 6;
+    uint32_t m = 0;
+    float s = 0.0f;
+    const bool sums = a.part_sum && first == 0;
+    if (c < a.cols) {
+      for (uint32_t k = part; k < a.chunks; k += 4) {
+        const uint64_t at = (uint64_t)k * a.cols + c;
+        if (a.part_max) m = max(m, a.part_max[at]);
+        if (sums) s += a.part_sum[at];
+      }
+    }
+    found[part][threadIdx.x & 63] = m;
+    added[part][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      const uint32_t t = threadIdx.x;
+      m = max(max(found[0][t], found[1][t]), max(found[2][t], found[3][t]));
+      float scale, inv;
+      scale_of(__uint_as_float(m), scale, inv);
+      factor[t] = inv;
+      if (first == 0 && c < a.cols) {
+        if (a.part_max) a.col_scale[c] = scale;
+        if (sums) a.col_sum[c] = (added[0][t] + added[1][t]) + (added[2][t] + added[3][t]);
+      }
+    }
+    __syncthreads();
+  }
+  if (!a.part_max) return;
+  const uint32_t cx = threadIdx.x & 7, ry = threadIdx.x >> 3, c = c0 + 8 * cx;
+  const uint32_t iteration = STOCHASTIC ? draw_iteration(a.draws) : 0;
+  float inv[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) inv[i] = factor[8 * cx + i];
+  const uint32_t end = min(first + kTileRows, a.rows);
+  // word w of column n: the 16-byte places of a column change with its number, so that eight threads' words do not meet
+  auto at = [&](uint32_t n, uint32_t w) { return 32 * n + 4 * ((w >> 2) ^ (n >> 3 & 7)) + (w & 3); };
+  for (uint32_t r0 = first; r0 < end; r0 += 128) {
+    const uint32_t r = r0 + 4 * ry;
+    if (c < a.cols && r < a.rows) {
+      Eight<TYPE> x[4] = {};
+      HalfWords h[4] = {};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (r + i < a.rows) x[i].load(element_at<TYPE>(a.x, a.ld, r + i, c), a.cols - c, a.wide);
+      if constexpr (STOCHASTIC) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = draw_block(a.draws, iteration, r + i, c / 8);
+      }
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        float t[4];
+        uint32_t left[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          t[i] = x[i].value(n) * inv[n];
+          left[i] = draw_left(h[i], n);
+        }
+        tile[at(8 * cx + n, ry)] = STOCHASTIC ? stochastic_levels(t, left) : nearest_levels(t);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t p = 0; p < 2; ++p) {
+      const uint32_t n = 32 * p + threadIdx.x / 8, row = r0 + 16 * (threadIdx.x & 7);
+      if (c0 + n < a.cols && row < a.rows) {
+        const uint4 v = *reinterpret_cast<const uint4*>(&tile[at(n, 4 * (threadIdx.x & 7))]);
+        int8_t* out = a.q_cols + ((c0 + n) * a.q_cols_ld + row);
+        if (a.rows - row >= 16) {
+          *reinterpret_cast<uint4*>(out) = v;
+        } else {
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (uint32_t i = 0; i < 15; ++i)
+            if (row + i < a.rows) out[i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+        }
+      }
+    }
+    __syncthreads();
   }
 }
 
 }  // namespace
 
-void plan_columns(uint32_t rows, uint32_t cols, uint32_t& chunks, uint32_t& chunk_rows) {
-  const uint32_t strips = (cols + kStripCols - 1) / kStripCols;
-  const uint32_t want = strips ? (1024 + strips - 1) / strips : 1;
-  chunk_rows = rows / want < 32 ? 32 : (rows + want - 1) / want;
+void plan_columns(uint32_t rows, uint32_t cols, uint32_t& strip_lanes, uint32_t& chunks, uint32_t& chunk_rows) {
+  strip_lanes = 16;
+  while (strip_lanes > 1 && 4 * strip_lanes >= cols) strip_lanes /= 2;   // narrow matrices: more rows side by side
+  const uint64_t strips = (cols + 8ull * strip_lanes - 1) / (8 * strip_lanes);
+  // about 1024 workgroups, 64 chunks at most (each is read again by every tile of the second launch), and eight rows
+  // at least to every thread
+  const uint64_t want = strips ? (1024 + strips - 1) / strips : 1;
+  const uint64_t least = 8ull * (256 / strip_lanes);
+  const uint64_t each = (rows + (want < 64 ? want : 64) - 1) / (want < 64 ? want : 64);
+  chunk_rows = (uint32_t)(each < least ? least : each);
   chunks = (rows + chunk_rows - 1) / chunk_rows;
 }
 
-hipError_t launch_quantize_rows(const QuantizeArgs& a, uint32_t type, hipStream_t st) {
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.rows), dim3(256), 0, st, a); };
-  if (type == QSGD_TYPE_F32) go(k_quantize_rows<QSGD_TYPE_F32>);
-  else if (type == QSGD_TYPE_BF16) go(k_quantize_rows<QSGD_TYPE_BF16>);
-  else go(k_quantize_rows<QSGD_TYPE_F16>);
-  return hipGetLastError();
-}
-
-hipError_t launch_column_max(const QuantizeArgs& a, uint32_t type, hipStream_t st) {
-  const dim3 grid((a.cols + kStripCols - 1) / kStripCols, a.chunks);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
-  if (a.chunks == 0) {}
-  else if (type == QSGD_TYPE_F32) go(k_column_max<QSGD_TYPE_F32>);
-  else if (type == QSGD_TYPE_BF16) go(k_column_max<QSGD_TYPE_BF16>);
-  else go(k_column_max<QSGD_TYPE_F16>);
-  if (const hipError_t e = hipGetLastError()) return e;
-  hipLaunchKernelGGL(k_column_scale, dim3((a.cols + 255) / 256), dim3(256), 0, st, a);
-  return hipGetLastError();
-}
-
-hipError_t launch_quantize_columns(const QuantizeArgs& a, uint32_t type, hipStream_t st) {
-  const uint64_t tiles = (uint64_t)((a.cols + kTileCols - 1) / kTileCols) * ((a.rows + kTileRows - 1) / kTileRows);
-  if (tiles == 0) return hipSuccess;
-  if (tiles > 0x7FFFFFFFull) return hipErrorInvalidValue;
-  const dim3 grid((uint32_t)tiles);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a); };
-  if (type == QSGD_TYPE_F32) go(k_quantize_columns<QSGD_TYPE_F32>);
-  else if (type == QSGD_TYPE_BF16) go(k_quantize_columns<QSGD_TYPE_BF16>);
-  else go(k_quantize_columns<QSGD_TYPE_F16>);
+hipError_t launch_quantize(QuantizeJobs& jobs, uint32_t type, bool stochastic, hipStream_t st, bool second) {
+  uint64_t blocks = 0;
+  for (uint32_t j = 0; j < jobs.count; ++j) {
+    QuantizeArgs& a = jobs.job[j];
+    if (second) {
+      const bool any = a.chunks && (a.part_max || a.part_sum);
+      const uint64_t down = a.part_max ? (a.rows + kTileRows - 1) / kTileRows : 1;
+      const uint64_t n = a.part_max || a.part_sum ? (uint64_t)((a.cols + 63) / 64) * (any ? down : 1) : 0;
+      if (n > 0x7FFFFFFFull) return hipErrorInvalidValue;
+      a.tile_blocks = (uint32_t)n;
+      blocks += n;
+    } else {
+      a.row_lanes = a.cols <= 8 * 64 * kHeld && a.rows >= 1024 ? 64 : 256;   // a wavefront to a row, or four
+      a.row_blocks = !a.q_rows && !a.row_scale ? 0 : a.row_lanes == 64 ? (a.rows + 3) / 4 : a.rows;
+      a.max_blocks = a.part_max || a.part_sum ? (a.cols + 8 * a.strip_lanes - 1) / (8 * a.strip_lanes) * a.chunks : 0;
+      blocks += (uint64_t)a.row_blocks + a.max_blocks;
+    }
+  }
+  if (blocks == 0) return hipSuccess;
+  if (blocks > 0x7FFFFFFFull) return hipErrorInvalidValue;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(256), 0, st, jobs); };
+  auto pick = [&](auto type_c) {
+    constexpr uint32_t T = decltype(type_c)::value;
+    if (second) stochastic ? go(k_quantize_columns<T, true>) : go(k_quantize_columns<T, false>);
+    else stochastic ? go(k_quantize_rows<T, true>) : go(k_quantize_rows<T, false>);
+  };
+  if (type == QSGD_TYPE_F32) pick(std::integral_constant<uint32_t, QSGD_TYPE_F32>{});
+  else if (type == QSGD_TYPE_BF16) pick(std::integral_constant<uint32_t, QSGD_TYPE_BF16>{});
+  else pick(std::integral_constant<uint32_t, QSGD_TYPE_F16>{});
   return hipGetLastError();
 }
 
