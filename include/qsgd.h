@@ -253,8 +253,7 @@ int qsgd_pipeline_step(qsgd_pipeline *pl, const qsgd_params *p, uint64_t chunk_e
 #define QSGD_ROUND_STOCHASTIC 1u /* to one of the two levels around the value, unbiased      */
 
 /* A matrix in device memory: element (r, c) is at data_dev[r * ld + c].  rows, cols < 2^31,
- * rows * ld < 2^46.  ld >= cols; the data are aligned to their element's size (rows that are 16
- * bytes apart modulo 16 and start at a multiple of 16 bytes are faster).  Matrices of QSGD_TYPE_I8
+ * rows * ld < 2^46.  ld >= cols; the data are aligned to their element's size.  Matrices of QSGD_TYPE_I8
  * are aligned to 16 bytes, ld is a multiple of 16, and the bytes of a row up to the next
  * multiple of 16 are readable; what stands there changes no result and is not written.
  * data_dev may be NULL where rows or cols is 0. */

@@ -32,11 +32,6 @@ bool sound(const qsgd_matrix* m, bool levels) {
 
 bool shaped(const qsgd_matrix* m, uint64_t rows, uint64_t cols) { return m->rows == rows && m->cols == cols; }
 
-// Every row starts at a multiple of 16 bytes.
-bool wide(const qsgd_matrix* m) {
-  return aligned(m->data_dev, 16) && (m->rows <= 1 || m->ld * size_of(m->type) % 16 == 0);
-}
-
 // Bytes [first, second) that a matrix covers.
 struct Span { uintptr_t from, to; };
 Span span(const qsgd_matrix* m) {
@@ -72,7 +67,7 @@ int dropout(const qsgd_draws* draws, float p, const qsgd_matrix* x, const qsgd_m
   if (residual && overlap(residual, y) && !same_place(residual, y)) return QSGD_ERR_INVALID_ARG;
   DropoutArgs a = {};
   if (int rc = draw_args(draws, x->rows, a.draws)) return rc;
-  if (x->rows * ((x->cols + 7) / 8) > (1ull << 40)) return QSGD_ERR_UNSUPPORTED;
+  if (x->rows * ((x->cols + 7) / 8) > 0xFFull << 31) return QSGD_ERR_UNSUPPORTED;
   if (x->rows == 0 || x->cols == 0) return QSGD_OK;
   a.x = x->data_dev; a.x_ld = x->ld;
   a.y = y->data_dev; a.y_ld = y->ld;
@@ -80,7 +75,6 @@ int dropout(const qsgd_draws* draws, float p, const qsgd_matrix* x, const qsgd_m
   a.rows = (uint32_t)x->rows; a.cols = (uint32_t)x->cols;
   a.drop = (uint32_t)std::nearbyint(65536.0 * (double)p);
   a.scale = a.drop == 65536 ? 0.0f : 65536.0f / (float)(65536 - a.drop);
-  a.wide = wide(x) && wide(y) && (!residual || wide(residual));
   ScopedTiming tm(name, st);
   return status(launch_dropout(a, x->type, st));
 }
@@ -104,7 +98,6 @@ QuantizeArgs job(const qsgd_matrix* x, const DrawArgs& draws) {
   QuantizeArgs q = {};
   q.x = x->data_dev; q.ld = x->ld;
   q.rows = (uint32_t)x->rows; q.cols = (uint32_t)x->cols;
-  q.wide = wide(x);
   q.draws = draws;
   return q;
 }

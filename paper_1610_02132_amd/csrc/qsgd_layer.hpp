@@ -70,12 +70,16 @@ template <uint32_t TYPE> struct Eight {
     if constexpr (kWords == 8) w[i] = b;
     else w[i >> 1] = i & 1 ? w[i >> 1] | b << 16 : b;   // (in ascending order)
   }
-  // Elements [0, n) of p; the others read as zero.  `wide`: p is aligned to 16 bytes.
-  __device__ __forceinline__ void load(const void* p, uint32_t n, bool wide) {
-    if (wide && n >= 8) {
+  // Elements [0, n) of p, aligned to their own size (the machine loads 16 bytes from any address); the others read as
+  // zero.  STREAM: past the caches, for matrices that they do not hold.
+  using Words = __attribute__((ext_vector_type(4), aligned(sizeof(typename Element<TYPE>::bits)))) uint32_t;
+  template <bool STREAM = false>
+  __device__ __forceinline__ void load(const void* p, uint32_t n) {
+    if (n >= 8) {
 #pragma unroll
       for (int j = 0; j < kWords; j += 4) {
-        const uint4 v = reinterpret_cast<const uint4*>(p)[j / 4];
+        const Words* from = reinterpret_cast<const Words*>(p) + j / 4;
+        const Words v = STREAM ? __builtin_nontemporal_load(from) : *from;
         w[j] = v.x; w[j + 1] = v.y; w[j + 2] = v.z; w[j + 3] = v.w;
       }
     } else {
@@ -84,15 +88,20 @@ template <uint32_t TYPE> struct Eight {
       for (int i = 0; i < 8; ++i) set(i, (uint32_t)i < n ? e[i] : 0u);
     }
   }
-  __device__ __forceinline__ void store(void* p, uint32_t n, bool wide) const {
-    if (wide && n >= 8) {
+  template <bool STREAM = false>
+  __device__ __forceinline__ void store(void* p, uint32_t n) const {
+    if (n >= 8) {
 #pragma unroll
-      for (int j = 0; j < kWords; j += 4)
-        reinterpret_cast<uint4*>(p)[j / 4] = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+      for (int j = 0; j < kWords; j += 4) {
+        Words* to = reinterpret_cast<Words*>(p) + j / 4;
+        const Words v = {w[j], w[j + 1], w[j + 2], w[j + 3]};
+        if constexpr (STREAM) __builtin_nontemporal_store(v, to);
+        else *to = v;
+      }
     } else {
       auto* e = reinterpret_cast<typename Element<TYPE>::bits*>(p);
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 7; ++i)
         if ((uint32_t)i < n) e[i] = (typename Element<TYPE>::bits)bits(i);
     }
   }
@@ -115,20 +124,17 @@ struct DropoutArgs {
   uint32_t rows, cols;
   uint32_t drop;              // D: draws below it drop the element
   float scale;                // 65536 / (65536 - D), or 0
-  bool wide;                  // every row of every matrix is aligned to 16 bytes
   DrawArgs draws;
 };
 hipError_t launch_dropout(const DropoutArgs& a, uint32_t type, hipStream_t st);
 
 // ---- quantizer ---------------------------------------------------------------------
 constexpr float kTinyMax = 0x1p-119f;   // rows whose largest magnitude is below it count as zero: 127 / m and m / 127 stay normal
-constexpr uint32_t kTileRows = 512;     // rows that a workgroup of the column form takes
 
 struct QuantizeArgs {
   const void* x;
   uint64_t ld;
   uint32_t rows, cols;
-  bool wide;                  // every row of x is aligned to 16 bytes
   DrawArgs draws;
   int8_t* q_rows; uint64_t q_rows_ld; float* row_scale;   // row_scale: or null
   int8_t* q_cols; uint64_t q_cols_ld; float* col_scale;
@@ -139,6 +145,8 @@ struct QuantizeArgs {
   float* col_sum;             // where the sums go
   // workgroups (launch_quantize)
   uint32_t row_lanes, row_blocks, max_blocks, tile_blocks;
+  bool stream;                // the second launch reads x past the caches
+  uint32_t tile_rows;         // rows that a workgroup of the second launch takes, a multiple of 128
 };
 struct QuantizeJobs { uint32_t count; QuantizeArgs job[3]; };
 // Lanes to a row of a strip of columns, rows of a chunk, and how many chunks there are.

@@ -91,13 +91,13 @@ __device__ __forceinline__ void rows_block(const QuantizeArgs& a, uint32_t first
   for (int u = 0; u < kHeld; ++u) {
     const uint32_t c8 = u * LANES + lane;
     if (have && c8 < c8s) {
-      held[u].load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8, a.wide);
+      held[u].load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8);
       most.add(held[u]);
     }
   }
   for (uint32_t c8 = kHeld * LANES + lane; have && c8 < c8s; c8 += LANES) {
     Eight<TYPE> x;
-    x.load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8, a.wide);
+    x.load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8);
     most.add(x);
   }
   uint32_t m = 0;
@@ -147,7 +147,7 @@ __device__ __forceinline__ void rows_block(const QuantizeArgs& a, uint32_t first
   }
   for (uint32_t c8 = kHeld * LANES + lane; c8 < c8s; c8 += LANES) {
     Eight<TYPE> x;
-    x.load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8, a.wide);
+    x.load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8);
     put(x, c8);
   }
 }
@@ -174,13 +174,13 @@ __device__ __forceinline__ void columns_block(const QuantizeArgs& a, uint32_t bl
     for (; r + 3 * parts < r1; r += 4 * parts) {   // (four rows on their way)
       Eight<TYPE> x[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) x[u].load(element_at<TYPE>(a.x, a.ld, r + u * parts, c), a.cols - c, a.wide);
+      for (int u = 0; u < 4; ++u) x[u].load(element_at<TYPE>(a.x, a.ld, r + u * parts, c), a.cols - c);
 #pragma unroll
       for (int u = 0; u < 4; ++u) take(x[u]);
     }
     for (; r < r1; r += parts) {
       Eight<TYPE> x;
-      x.load(element_at<TYPE>(a.x, a.ld, r, c), a.cols - c, a.wide);
+      x.load(element_at<TYPE>(a.x, a.ld, r, c), a.cols - c);
       take(x);
     }
   }
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
   uint32_t block = blockIdx.x, j = 0;
   while (block >= jobs.job[j].tile_blocks) block -= jobs.job[j++].tile_blocks;   // (the grid is their sum)
   const QuantizeArgs& a = jobs.job[j];
-  const uint32_t strips = (a.cols + 63) / 64, c0 = block % strips * 64, first = block / strips * kTileRows;
+  const uint32_t strips = (a.cols + 63) / 64, c0 = block % strips * 64, first = block / strips * a.tile_rows;
   {   // the chunks' maxima and sums, by four threads to a column
     const uint32_t c = c0 + (threadIdx.x & 63), part = threadIdx.x >> 6;
     uint32_t m = 0;
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
   float inv[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) inv[i] = factor[8 * cx + i];
-  const uint32_t end = min(first + kTileRows, a.rows);
+  const uint32_t end = min(first + a.tile_rows, a.rows);
   // word w of column n: the 16-byte places of a column change with its number, so that eight threads' words do not meet
   auto at = [&](uint32_t n, uint32_t w) { return 32 * n + 4 * ((w >> 2) ^ (n >> 3 & 7)) + (w & 3); };
   for (uint32_t r0 = first; r0 < end; r0 += 128) {
@@ -291,7 +291,11 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
       HalfWords h[4] = {};
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (r + i < a.rows) x[i].load(element_at<TYPE>(a.x, a.ld, r + i, c), a.cols - c, a.wide);
+        if (r + i < a.rows) {
+          const void* p = element_at<TYPE>(a.x, a.ld, r + i, c);
+          if (a.stream) x[i].template load<true>(p, a.cols - c);
+          else x[i].load(p, a.cols - c);
+        }
       if constexpr (STOCHASTIC) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = draw_block(a.draws, iteration, r + i, c / 8);
@@ -350,8 +354,16 @@ hipError_t launch_quantize(QuantizeJobs& jobs, uint32_t type, bool stochastic, h
     QuantizeArgs& a = jobs.job[j];
     if (second) {
       const bool any = a.chunks && (a.part_max || a.part_sum);
-      const uint64_t down = a.part_max ? (a.rows + kTileRows - 1) / kTileRows : 1;
-      const uint64_t n = a.part_max || a.part_sum ? (uint64_t)((a.cols + 63) / 64) * (any ? down : 1) : 0;
+      const uint64_t strips = (a.cols + 63) / 64;
+      // the last reading of a matrix that L2 does not hold goes past the caches (gradients of 8192 tokens, 4096 -> 4096
+      // bf16: 360 us without, 347 with)
+      a.stream = (uint64_t)a.rows * a.cols * (type == QSGD_TYPE_F32 ? 4 : 2) >= 32ull << 20;
+      // every workgroup reads the chunks' maxima: few rows to one only where there would be too few of them
+      // (2047 x 1001, both forms, the whole call: 128 rows 16.1 us, 512 rows 22.2; 8192 x 4096 the same)
+      a.tile_rows = 512;
+      while (a.tile_rows > 128 && strips * ((a.rows + a.tile_rows - 1) / a.tile_rows) < 1024) a.tile_rows /= 2;
+      const uint64_t down = a.part_max ? (a.rows + a.tile_rows - 1) / a.tile_rows : 1;
+      const uint64_t n = a.part_max || a.part_sum ? strips * (any ? down : 1) : 0;
       if (n > 0x7FFFFFFFull) return hipErrorInvalidValue;
       a.tile_blocks = (uint32_t)n;
       blocks += n;
