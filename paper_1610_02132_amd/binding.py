@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 CODE_SPARSE, CODE_DENSE, CODE_FIXED = 0, 1, 2
@@ -61,14 +62,9 @@ class Params:
                        self.stream_id, self.iteration, 0)
 
 
-class _Matrix(C.Structure):
-    _fields_ = [("data_dev", C.c_void_p), ("rows", C.c_uint64), ("cols", C.c_uint64),
-                ("ld", C.c_uint64), ("type", C.c_uint32), ("reserved", C.c_uint32)]
-
-
-class _Draws(C.Structure):
-    _fields_ = [("seed", C.c_uint64), ("stream_id", C.c_uint32), ("iteration", C.c_uint32),
-                ("row_base", C.c_uint32), ("reserved", C.c_uint32), ("iteration_dev", C.c_void_p)]
+# The bytes of struct qsgd_matrix and struct qsgd_draws (a ctypes structure takes three times as long to fill).
+_pack_matrix = struct.Struct("=QQQQII").pack
+_pack_draws = struct.Struct("=QIIIIQ").pack
 
 
 @dataclass
@@ -80,12 +76,14 @@ class Draws:
     row_base: int = 0
     iteration_dev: object = None
 
-    def c(self) -> _Draws:
+    def c(self) -> bytes:
+        """The bytes of a struct qsgd_draws."""
         t = self.iteration_dev
-        if t is not None and (not t.is_cuda or t.numel() != 1 or t.dtype.itemsize != 4 or t.dtype.is_floating_point):
+        if t is None:
+            return _pack_draws(self.seed, self.stream_id, self.iteration, self.row_base, 0, 0)
+        if not t.is_cuda or t.numel() != 1 or t.dtype.itemsize != 4 or t.dtype.is_floating_point:
             raise ValueError("iteration_dev must be a device tensor of one 32-bit integer")
-        return _Draws(self.seed, self.stream_id, self.iteration, self.row_base, 0,
-                      None if t is None else t.data_ptr())
+        return _pack_draws(self.seed, self.stream_id, self.iteration, self.row_base, 0, t.data_ptr())
 
 
 _lib = None
@@ -165,7 +163,7 @@ def _load():
     L.qsgd_pipeline_step.argtypes = [vp, PP, C.c_uint64, vp, C.c_uint32, C.c_float, vp, vp, sz,
                                      vp, vp, sz, vp]
     L.qsgd_pipeline_step.restype = C.c_int
-    PM, PD, u32, u64 = C.POINTER(_Matrix), C.POINTER(_Draws), C.c_uint32, C.c_uint64
+    PM, PD, u32, u64 = vp, vp, C.c_uint32, C.c_uint64   # (a structure, or its bytes)
     L.qsgd_dropout.argtypes = [PD, C.c_float, PM, PM, PM, vp]
     L.qsgd_dropout_backward.argtypes = [PD, C.c_float, PM, PM, vp]
     L.qsgd_quantize_workspace_bytes.argtypes = [u64, u64]
@@ -531,56 +529,65 @@ _types = None   # torch dtype -> QSGD_TYPE_*
 
 
 def _matrix(t, what: str):
-    """A two-dimensional device tensor with contiguous rows as a qsgd_matrix (None for None)."""
-    global _types
+    """A two-dimensional device tensor with contiguous rows as the bytes of a qsgd_matrix (None for None)."""
     if t is None:
         return None
-    if _types is None:
-        import torch
-        _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int8: 3}
-    kind = _types.get(t.dtype)
+    kind = (_types or _load_types()).get(t.dtype)
     if kind is None:
         raise ValueError(f"{what} must be float32, bfloat16, float16 or int8")
-    if not t.is_cuda or t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{what} must be a device tensor of two dimensions")
-    rows, cols = t.shape
+    rows, cols = shape
     ld, step = t.stride()
-    if rows <= 1 and ld < cols:
-        ld = cols if kind != 3 else (cols + 15) // 16 * 16   # (a single row's stride means nothing)
-    if rows and cols and ((cols > 1 and step != 1) or ld < cols):
-        raise ValueError(f"{what} must have contiguous rows that do not overlap")
-    if kind == 3 and rows and cols:   # bytes up to the next multiple of 16 are read
-        if rows == 1 and ld % 16:
-            ld = (cols + 15) // 16 * 16
-        if t.storage_offset() + (rows - 1) * ld + (cols + 15) // 16 * 16 > t.untyped_storage().nbytes():
+    if kind == 3:
+        padded = (cols + 15) & ~15
+        if rows == 1 and (ld < cols or ld & 15):
+            ld = padded                                # (a single row's stride means nothing)
+        # bytes up to the next multiple of 16 are read
+        if cols & 15 and rows and t.storage_offset() + (rows - 1) * ld + padded > t.untyped_storage().nbytes():
             raise ValueError(f"{what}: its last row must be readable up to a multiple of 16 bytes")
-    return _Matrix(t.data_ptr(), rows, cols, max(ld, cols), kind, 0)
+    elif rows <= 1 and ld < cols:
+        ld = cols
+    if (step != 1 and cols > 1 and rows) or ld < cols:
+        if rows and cols:
+            raise ValueError(f"{what} must have contiguous rows that do not overlap")
+        ld = cols
+    return _pack_matrix(t.data_ptr(), rows, cols, ld, kind, 0)
+
+
+def _load_types():
+    global _types
+    import torch
+    _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int8: 3}
+    return _types
 
 
 def _vector(t, n: int, what: str):
     """Address of a device tensor of n float32 (None for None)."""
     if t is None:
         return None
-    if t.dtype.itemsize != 4 or not t.dtype.is_floating_point or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+    types = _types or _load_types()
+    if types.get(t.dtype) != 0 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous device tensor of {n} float32")
     return t.data_ptr()
 
 
-def _ref(c):
-    return None if c is None else C.byref(c)
+def _draws(d):
+    return None if d is None else d.c()
 
 
 def qsgd_dropout(draws: Draws, p: float, x, y, residual=None, stream=None) -> None:
     """Queues y = residual + dropout(x); y may be x or residual."""
-    rc = _load().qsgd_dropout(C.byref(draws.c()), p, _ref(_matrix(x, "x")), _ref(_matrix(residual, "residual")),
-                              _ref(_matrix(y, "y")), _stream(stream))
+    rc = _load().qsgd_dropout(_draws(draws), p, _matrix(x, "x"), _matrix(residual, "residual"),
+                              _matrix(y, "y"), _stream(stream))
     if rc:
         raise QsgdError(rc, "qsgd_dropout")
 
 
 def qsgd_dropout_backward(draws: Draws, p: float, dy, dx, stream=None) -> None:
     """Queues dx = the gradient of qsgd_dropout's x; dx may be dy."""
-    rc = _load().qsgd_dropout_backward(C.byref(draws.c()), p, _ref(_matrix(dy, "dy")), _ref(_matrix(dx, "dx")),
+    rc = _load().qsgd_dropout_backward(_draws(draws), p, _matrix(dy, "dy"), _matrix(dx, "dx"),
                                        _stream(stream))
     if rc:
         raise QsgdError(rc, "qsgd_dropout_backward")
@@ -594,11 +601,11 @@ def qsgd_quantize(draws, x, rows=None, row_scale=None, columns=None, column_scal
                   rounding: int = ROUND_NEAREST, stream=None) -> None:
     """Queues the levels of x by rows (int8, x's shape) and / or by columns (int8, transposed), and their scales.
     draws: Draws, or None for ROUND_NEAREST."""
-    mx = _matrix(x, "x")
+    mx, (n, d) = _matrix(x, "x"), x.shape
     wp, wbytes = _dev(workspace, "workspace")
-    rc = _load().qsgd_quantize(_ref(draws.c() if draws is not None else None), rounding, _ref(mx),
-                               _ref(_matrix(rows, "rows")), _vector(row_scale, mx.rows, "row_scale"),
-                               _ref(_matrix(columns, "columns")), _vector(column_scale, mx.cols, "column_scale"),
+    rc = _load().qsgd_quantize(_draws(draws), rounding, mx,
+                               _matrix(rows, "rows"), _vector(row_scale, n, "row_scale"),
+                               _matrix(columns, "columns"), _vector(column_scale, d, "column_scale"),
                                wp, wbytes, _stream(stream))
     if rc:
         raise QsgdError(rc, "qsgd_quantize")
@@ -610,11 +617,11 @@ def qsgd_int_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
 
 def qsgd_int_matmul(a, a_scale, b, b_scale, y, bias=None, workspace=None, stream=None) -> None:
     """Queues y = (a b^T) * a_scale[:, None] * b_scale + bias, a (M x K) and b (N x K) int8."""
-    ma, mb = _matrix(a, "a"), _matrix(b, "b")
+    ma, mb, N = _matrix(a, "a"), _matrix(b, "b"), b.shape[0]
     wp, wbytes = _dev(workspace, "workspace")
-    rc = _load().qsgd_int_matmul(_ref(ma), _vector(a_scale, ma.rows, "a_scale"), _ref(mb),
-                                 _vector(b_scale, mb.rows, "b_scale"), _vector(bias, mb.rows, "bias"),
-                                 _ref(_matrix(y, "y")), wp, wbytes, _stream(stream))
+    rc = _load().qsgd_int_matmul(ma, _vector(a_scale, a.shape[0], "a_scale"), mb,
+                                 _vector(b_scale, N, "b_scale"), _vector(bias, N, "bias"),
+                                 _matrix(y, "y"), wp, wbytes, _stream(stream))
     if rc:
         raise QsgdError(rc, "qsgd_int_matmul")
 
@@ -626,11 +633,11 @@ def qsgd_linear_forward_workspace_bytes(tokens: int, outputs: int, inputs: int) 
 def qsgd_linear_forward(draws, x, w, w_scale, y, bias=None, workspace=None, rounding: int = ROUND_NEAREST,
                         stream=None) -> None:
     """Queues y = Q(x) w^T * w_scale + bias, w (outputs x inputs) int8 as qsgd_quantize left it by rows."""
-    mw = _matrix(w, "w")
+    mw, N = _matrix(w, "w"), w.shape[0]
     wp, wbytes = _dev(workspace, "workspace")
-    rc = _load().qsgd_linear_forward(_ref(draws.c() if draws is not None else None), rounding,
-                                     _ref(_matrix(x, "x")), _ref(mw), _vector(w_scale, mw.rows, "w_scale"),
-                                     _vector(bias, mw.rows, "bias"), _ref(_matrix(y, "y")), wp, wbytes,
+    rc = _load().qsgd_linear_forward(_draws(draws), rounding,
+                                     _matrix(x, "x"), mw, _vector(w_scale, N, "w_scale"),
+                                     _vector(bias, N, "bias"), _matrix(y, "y"), wp, wbytes,
                                      _stream(stream))
     if rc:
         raise QsgdError(rc, "qsgd_linear_forward")
@@ -643,11 +650,11 @@ def qsgd_linear_backward_workspace_bytes(tokens: int, outputs: int, inputs: int)
 def qsgd_linear_backward(draws, x, w, dy, dx=None, dw=None, db=None, workspace=None,
                          rounding: int = ROUND_NEAREST, stream=None) -> None:
     """Queues the gradients that are asked for: dx (x's type), dw and db (float32)."""
-    mw = _matrix(w, "w")
+    mw, N = _matrix(w, "w"), w.shape[0]
     wp, wbytes = _dev(workspace, "workspace")
-    rc = _load().qsgd_linear_backward(_ref(draws.c() if draws is not None else None), rounding,
-                                      _ref(_matrix(x, "x")), _ref(mw), _ref(_matrix(dy, "dy")),
-                                      _ref(_matrix(dx, "dx")), _ref(_matrix(dw, "dw")),
-                                      _vector(db, mw.rows, "db"), wp, wbytes, _stream(stream))
+    rc = _load().qsgd_linear_backward(_draws(draws), rounding,
+                                      _matrix(x, "x"), mw, _matrix(dy, "dy"),
+                                      _matrix(dx, "dx"), _matrix(dw, "dw"),
+                                      _vector(db, N, "db"), wp, wbytes, _stream(stream))
     if rc:
         raise QsgdError(rc, "qsgd_linear_backward")

@@ -133,8 +133,7 @@ int quantize(QuantizeJobs& jobs, uint32_t type, uint32_t rounding, hipStream_t s
 constexpr uint64_t kMostLd = 1ull << 23;
 constexpr uint64_t kMostResults = 1ull << 38;   // of one product: workgroups are counted in 31 bits
 
-int product(ProductArgs& p, uint8_t* ws, hipStream_t st) {
-  const ProductPlan plan = plan_product(p.M, p.N, p.K);
+int product(ProductArgs& p, const ProductPlan& plan, uint8_t* ws, hipStream_t st) {
   p.splits = plan.splits; p.split_k = plan.split_k;
   p.part = plan.bytes ? reinterpret_cast<int32_t*>(ws) : nullptr;
   p.wide = p.part ? p.N % 4 == 0 : aligned(p.y, 16) && (p.M <= 1 || p.y_ld * size_of(p.type) % 16 == 0);
@@ -154,21 +153,37 @@ uint64_t levels_ld(uint64_t k) { return (k + 127) / 128 * 128; }
 
 bool in_range(uint64_t a, uint64_t b, uint64_t c) { return a < 1ull << 31 && b < 1ull << 31 && c < 1ull << 31; }
 
-uint64_t product_bytes(uint64_t M, uint64_t N, uint64_t K) {
-  if (!M || !N || M >= kMostResults / N || K >= kMostLd) return 0;   // (nothing to do, or refused)
-  return plan_product((uint32_t)M, (uint32_t)N, (uint32_t)K).bytes;
+ProductPlan product_plan(uint64_t M, uint64_t N, uint64_t K) {
+  if (!M || !N || M >= kMostResults / N || K >= kMostLd) return {};   // (nothing to do, or refused)
+  return plan_product((uint32_t)M, (uint32_t)N, (uint32_t)K);
 }
+uint64_t product_bytes(uint64_t M, uint64_t N, uint64_t K) { return product_plan(M, N, K).bytes; }
 
 bool room(const void* ws, size_t have, uint64_t need) { return need == 0 || (ws && aligned(ws, 16) && have >= need); }
 
 // Why a workspace is refused.
 int no_room(const void* ws, uint64_t need) { return need && (!ws || !aligned(ws, 16)) ? QSGD_ERR_INVALID_ARG : QSGD_ERR_CAPACITY; }
 
+// Workspace of the layer: x's levels and scales, then what the product needs.
+struct ForwardSpace {
+  ProductPlan plan;
+  uint64_t scale, rest, bytes;
+};
+ForwardSpace forward_space(uint64_t M, uint64_t N, uint64_t K) {
+  ForwardSpace s = {};
+  s.plan = product_plan(M, N, K);
+  s.scale = padded(M * levels_ld(K));
+  s.rest = s.scale + padded(4 * M);
+  s.bytes = s.rest + s.plan.bytes;
+  return s;
+}
+
 // Workspace of the layer's gradients: levels and scales of its operands, the columns' maxima and sums, and what the
 // products need, one after the other.
 struct BackwardSpace {
   uint64_t dy_rows, dy_row_scale, w_cols, w_scale, dy_cols, dy_col_scale, x_cols, x_scale;
   uint64_t dy_space, w_space, x_space, rest, bytes;
+  ProductPlan dx, dw;
 };
 BackwardSpace backward_space(uint64_t M, uint64_t N, uint64_t K) {
   BackwardSpace s = {};
@@ -181,7 +196,9 @@ BackwardSpace backward_space(uint64_t M, uint64_t N, uint64_t K) {
   s.dy_space = take(column_space(M, N).bytes);
   s.w_space = take(column_space(N, K).bytes);
   s.x_space = take(column_space(M, K).bytes);
-  s.rest = take(std::max(product_bytes(M, K, N), product_bytes(N, K, M)));
+  s.dx = product_plan(M, K, N);
+  s.dw = product_plan(N, K, M);
+  s.rest = take(std::max(s.dx.bytes, s.dw.bytes));
   s.bytes = at;
   return s;
 }
@@ -237,7 +254,8 @@ int qsgd_int_matmul(const qsgd_matrix* a, const float* a_scale_dev, const qsgd_m
     return QSGD_ERR_INVALID_ARG;
   if (a->ld >= kMostLd || b->ld >= kMostLd || too_many(y->rows, y->cols)) return QSGD_ERR_UNSUPPORTED;
   if (y->rows == 0 || y->cols == 0) return QSGD_OK;
-  const uint64_t need = product_bytes(a->rows, b->rows, a->cols);
+  const ProductPlan plan = product_plan(a->rows, b->rows, a->cols);
+  const uint64_t need = plan.bytes;
   if (!room(workspace_dev, workspace_bytes, need)) return no_room(workspace_dev, need);
   ProductArgs p = {};
   p.a = reinterpret_cast<const int8_t*>(a->data_dev); p.a_ld = a->ld;
@@ -245,12 +263,11 @@ int qsgd_int_matmul(const qsgd_matrix* a, const float* a_scale_dev, const qsgd_m
   p.M = (uint32_t)a->rows; p.N = (uint32_t)b->rows; p.K = (uint32_t)a->cols;
   p.a_scale = a_scale_dev; p.b_scale = b_scale_dev; p.bias = bias_dev;
   p.y = y->data_dev; p.y_ld = y->ld; p.type = y->type;
-  return product(p, reinterpret_cast<uint8_t*>(workspace_dev), reinterpret_cast<hipStream_t>(hip_stream));
+  return product(p, plan, reinterpret_cast<uint8_t*>(workspace_dev), reinterpret_cast<hipStream_t>(hip_stream));
 }
 
 size_t qsgd_linear_forward_workspace_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs) {
-  if (!in_range(tokens, outputs, inputs)) return 0;
-  return padded(tokens * levels_ld(inputs)) + padded(4 * tokens) + product_bytes(tokens, outputs, inputs);
+  return in_range(tokens, outputs, inputs) ? forward_space(tokens, outputs, inputs).bytes : 0;
 }
 
 int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix* x, const qsgd_matrix* w,
@@ -265,14 +282,14 @@ int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_m
   if (rounding == QSGD_ROUND_STOCHASTIC || draws)
     if (int rc = draw_args(draws, x->rows, d)) return rc;
   if (y->rows == 0 || y->cols == 0) return QSGD_OK;
-  const uint64_t need = qsgd_linear_forward_workspace_bytes(x->rows, w->rows, x->cols);
-  if (!room(workspace_dev, workspace_bytes, need)) return no_room(workspace_dev, need);
+  const ForwardSpace s = forward_space(x->rows, w->rows, x->cols);
+  if (!room(workspace_dev, workspace_bytes, s.bytes)) return no_room(workspace_dev, s.bytes);
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   uint8_t* ws = reinterpret_cast<uint8_t*>(workspace_dev);
-  const uint64_t ld = levels_ld(x->cols), scale_at = padded(x->rows * ld), rest = scale_at + padded(4 * x->rows);
+  const uint64_t ld = levels_ld(x->cols);
   QuantizeJobs jobs = {1, {job(x, d)}};
   QuantizeArgs& q = jobs.job[0];
-  want_rows(q, reinterpret_cast<int8_t*>(ws), ld, reinterpret_cast<float*>(ws + scale_at));
+  want_rows(q, reinterpret_cast<int8_t*>(ws), ld, reinterpret_cast<float*>(ws + s.scale));
   if (int rc = quantize(jobs, x->type, rounding, st)) return rc;
   ProductArgs p = {};
   p.a = q.q_rows; p.a_ld = ld;
@@ -280,7 +297,7 @@ int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_m
   p.M = (uint32_t)x->rows; p.N = (uint32_t)w->rows; p.K = (uint32_t)x->cols;
   p.a_scale = q.row_scale; p.b_scale = w_scale_dev; p.bias = bias_dev;
   p.y = y->data_dev; p.y_ld = y->ld; p.type = y->type;
-  return product(p, ws + rest, st);
+  return product(p, s.plan, ws + s.rest, st);
 }
 
 size_t qsgd_linear_backward_workspace_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs) {
@@ -341,7 +358,7 @@ int qsgd_linear_backward(const qsgd_draws* draws, uint32_t rounding, const qsgd_
     p.M = (uint32_t)N; p.N = (uint32_t)K; p.K = (uint32_t)M;
     p.a_scale = scales(s.dy_col_scale); p.b_scale = scales(s.x_scale);
     p.y = dw->data_dev; p.y_ld = dw->ld; p.type = QSGD_TYPE_F32;
-    if (int rc = product(p, ws + s.rest, st)) return rc;
+    if (int rc = product(p, s.dw, ws + s.rest, st)) return rc;
   }
   if (want_dx) {
     ProductArgs p = {};
@@ -349,7 +366,7 @@ int qsgd_linear_backward(const qsgd_draws* draws, uint32_t rounding, const qsgd_
     p.M = (uint32_t)M; p.N = (uint32_t)K; p.K = (uint32_t)N;
     p.a_scale = scales(s.dy_row_scale); p.b_scale = scales(s.w_scale);
     p.y = dx->data_dev; p.y_ld = dx->ld; p.type = dx->type;
-    if (int rc = product(p, ws + s.rest, st)) return rc;
+    if (int rc = product(p, s.dx, ws + s.rest, st)) return rc;
   }
   return QSGD_OK;
 }

@@ -1,7 +1,7 @@
 """The operators of a layer in 8 bits against plain forms in 64 bits: sizes that end inside a vector, a
 draw block or a tile, strides and alignments, empty and non-finite rows, every type and form."""
-import ctypes as C
 import itertools
+import struct
 
 import numpy as np
 import pytest
@@ -616,7 +616,7 @@ def test_the_c_abi_takes_a_null_residual_and_counts_rows_apart():
     L = binding._load()
     x = torch.ones(1, 40, device="cuda")
     y = torch.zeros(1, 40, device="cuda")
-    mx, my = binding._Matrix(x.data_ptr(), 1, 40, 1000, 0, 0), binding._Matrix(y.data_ptr(), 1, 40, 40, 0, 0)
-    assert L.qsgd_dropout(C.byref(D.c()), 0.5, C.byref(mx), None, C.byref(my), None) == 0
+    matrix = lambda t, ld: struct.pack("=QQQQII", t.data_ptr(), 1, 40, ld, 0, 0)  # noqa: E731  (struct qsgd_matrix)
+    assert L.qsgd_dropout(D.c(), 0.5, matrix(x, 1000), None, matrix(y, 40), None) == 0
     torch.cuda.synchronize()
     R.check(y, *R.dropout(D, 0.5, x))

@@ -1,7 +1,7 @@
 """What the operators of a layer in 8 bits refuse, on the host before anything is queued, and the sizes of
 their workspaces.  Addresses are made up: a refused call looks at no memory."""
-import ctypes as C
 import os
+import struct
 
 import pytest
 
@@ -21,18 +21,15 @@ def b():
 
 
 def mat(b, at, rows, cols, kind=F32, ld=None, reserved=0):
-    return b._Matrix(at, rows, cols, cols if ld is None else ld, kind, reserved)
+    return struct.pack("=QQQQII", at, rows, cols, cols if ld is None else ld, kind, reserved)   # struct qsgd_matrix
 
 
-def draws(b, **kw):
-    d = b.Draws(seed=1).c()
-    for k, v in kw.items():
-        setattr(d, k, v)
-    return d
+def draws(b, row_base=0, reserved=0, iteration_dev=0):
+    return struct.pack("=QIIIIQ", 1, 0, 0, row_base, reserved, iteration_dev)                   # struct qsgd_draws
 
 
 def ref(m):
-    return None if m is None else C.byref(m)
+    return m
 
 
 A, B, Y, Z = 0x10000000, 0x20000000, 0x30000000, 0x40000000   # far apart, aligned
