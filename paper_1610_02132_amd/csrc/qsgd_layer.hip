@@ -136,14 +136,29 @@ constexpr uint64_t kMostResults = 1ull << 38;   // of one product: workgroups ar
 int product(ProductArgs& p, const ProductPlan& plan, uint8_t* ws, hipStream_t st) {
   p.splits = plan.splits; p.split_k = plan.split_k;
   p.part = plan.bytes ? reinterpret_cast<int32_t*>(ws) : nullptr;
-  p.wide = p.part ? p.N % 4 == 0 : aligned(p.y, 16) && (p.M <= 1 || p.y_ld * size_of(p.type) % 16 == 0);
   {
     ScopedTiming tm("product", st);
-    if (int rc = status(launch_product(p, plan.kind, st))) return rc;
+    if (int rc = status(launch_products({{p}, 1, 0}, plan.kind, st))) return rc;
   }
   if (!p.part) return QSGD_OK;
   ScopedTiming tm("product_join", st);
   return status(launch_product_join(p, st));
+}
+
+// Two products whose plans are alike, each in one piece, can share a launch: plans[0] is the pair's then.  The tiles of 64
+// count as one kind, with four stages where all of them run at once.
+bool plan_pair(ProductPair& pair, ProductPlan (&plans)[2]) {
+  auto small = [](uint32_t kind) { return kind == kProductTile64 || kind == kProductTile64Deep; };
+  if (plans[0].splits != 1 || plans[1].splits != 1) return false;
+  if (small(plans[0].kind) && small(plans[1].kind)) {
+    uint64_t tiles = 0;
+    for (const ProductArgs& p : pair.of) tiles += (uint64_t)((p.M + 63) / 64) * ((p.N + 63) / 64);
+    plans[0].kind = tiles <= 512 ? kProductTile64Deep : kProductTile64;
+  } else if (plans[0].kind != plans[1].kind || plans[0].kind == kProductFew) {
+    return false;
+  }
+  for (ProductArgs& p : pair.of) { p.splits = 1; p.split_k = plans[0].split_k; }
+  return true;
 }
 
 bool too_many(uint64_t M, uint64_t N) { return N && M >= kMostResults / N; }
@@ -352,22 +367,30 @@ int qsgd_linear_backward(const qsgd_draws* draws, uint32_t rounding, const qsgd_
     want_columns(q, ws + s.x_space, levels(s.x_cols), levels_ld(M), scales(s.x_scale), nullptr);
   }
   if (int rc = quantize(jobs, x->type, rounding, st)) return rc;
+  ProductPair pair = {};
+  ProductPlan plans[2];
   if (want_dw) {
-    ProductArgs p = {};
+    ProductArgs& p = pair.of[pair.count];
     p.a = levels(s.dy_cols); p.b = levels(s.x_cols); p.a_ld = p.b_ld = levels_ld(M);
     p.M = (uint32_t)N; p.N = (uint32_t)K; p.K = (uint32_t)M;
     p.a_scale = scales(s.dy_col_scale); p.b_scale = scales(s.x_scale);
     p.y = dw->data_dev; p.y_ld = dw->ld; p.type = QSGD_TYPE_F32;
-    if (int rc = product(p, s.dw, ws + s.rest, st)) return rc;
+    plans[pair.count++] = s.dw;
   }
   if (want_dx) {
-    ProductArgs p = {};
+    ProductArgs& p = pair.of[pair.count];
     p.a = levels(s.dy_rows); p.b = levels(s.w_cols); p.a_ld = p.b_ld = levels_ld(N);
     p.M = (uint32_t)M; p.N = (uint32_t)K; p.K = (uint32_t)N;
     p.a_scale = scales(s.dy_row_scale); p.b_scale = scales(s.w_scale);
     p.y = dx->data_dev; p.y_ld = dx->ld; p.type = dx->type;
-    if (int rc = product(p, s.dx, ws + s.rest, st)) return rc;
+    plans[pair.count++] = s.dx;
   }
+  if (pair.count == 2 && plan_pair(pair, plans)) {   // both in one launch
+    ScopedTiming tm("product", st);
+    return status(launch_products(pair, plans[0].kind, st));
+  }
+  for (uint32_t i = 0; i < pair.count; ++i)
+    if (int rc = product(pair.of[i], plans[i], ws + s.rest, st)) return rc;
   return QSGD_OK;
 }
 

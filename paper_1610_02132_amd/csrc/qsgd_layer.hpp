@@ -163,7 +163,6 @@ struct ProductArgs {
   void* y;
   uint64_t y_ld;
   uint32_t type;
-  bool wide;                  // what is written (y, or the sums) has rows aligned to 16 bytes
   uint32_t splits, split_k;   // pieces of K and their length (a multiple of the tile's depth)
   int32_t* part;              // splits x M x N sums, or null with one piece
 };
@@ -175,8 +174,10 @@ enum ProductKind : uint32_t {
   kProductTile256,
 };
 struct ProductPlan { uint32_t kind, splits, split_k; uint64_t bytes; };
+// One product, or two that are planned alike and in one piece each.
+struct ProductPair { ProductArgs of[2]; uint32_t count, first; };
 ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K);
-hipError_t launch_product(const ProductArgs& a, uint32_t kind, hipStream_t st);
+hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t st);
 hipError_t launch_product_join(const ProductArgs& a, hipStream_t st);
 
 }  // namespace qsgd

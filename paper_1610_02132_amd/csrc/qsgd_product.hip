@@ -25,11 +25,11 @@ __device__ __forceinline__ float result(float sum, float s, float t, float bias)
   return s > kBigScale ? sum * (s * 0x1p-64f) * t * 0x1p64f + bias : __builtin_fmaf(sum * s, t, bias);
 }
 
-template <uint32_t TYPE>
 __device__ __forceinline__ void put(const ProductArgs& a, uint32_t m, uint32_t n, float sum) {
   const float v = result(sum, a.a_scale[m], a.b_scale[n], a.bias ? a.bias[n] : 0.0f);
-  *reinterpret_cast<typename Element<TYPE>::bits*>(element_at<TYPE>(a.y, a.y_ld, m, n)) =
-      (typename Element<TYPE>::bits)Element<TYPE>::narrow(v);
+  const uint64_t at = m * a.y_ld + n;
+  if (a.type == QSGD_TYPE_F32) reinterpret_cast<float*>(a.y)[at] = v;
+  else reinterpret_cast<uint16_t*>(a.y)[at] = (uint16_t)(a.type == QSGD_TYPE_BF16 ? Element<QSGD_TYPE_BF16>::narrow(v) : Element<QSGD_TYPE_F16>::narrow(v));
 }
 
 // 16 bytes of an operand from k on, those behind K zeroed.
@@ -101,13 +101,89 @@ __device__ __forceinline__ void weave() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-template <int MI, int NI, int STAGES, uint32_t TYPE>
-__global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductArgs a) {
+// A wavefront's results (32 MI rows of y from m0 on, 32 NI columns from n0 on) leave through LDS, 32 rows at a time, so that
+// a store covers whole lines, and a lane's columns, with their scales, are the same for every row.
+template <int MI, int NI, uint32_t ROOM, uint32_t TYPE>
+__device__ __forceinline__ void leave(const ProductArgs& a, const int16v (&acc)[MI][NI], uint8_t* stage, uint32_t m0, uint32_t n0) {
+  const uint32_t lane = threadIdx.x & 63;
+  constexpr uint32_t kSize = TYPE == QSGD_TYPE_F32 || TYPE == kSums ? 4 : 2, kPer = 16 / kSize;   // results of 16 bytes
+  constexpr uint32_t kRow = 32 * NI * 4 + 16, kChunks = 32 * NI / kPer, kRows = 64 / kChunks;      // rows that a store covers
+  static_assert(32 * kRow + 32 * MI * 4 <= ROOM, "");
+  float* x_scale = reinterpret_cast<float*>(stage + 32 * kRow);
+  const uint32_t n = n0 + lane % kChunks * kPer;
+  float w_scale[kPer], bias[kPer];
+  bool big = false;   // any row's scale is
+  if constexpr (TYPE != kSums) {
+#pragma unroll
+    for (uint32_t e = 0; e < kPer; ++e) {
+      const uint32_t at = min(n + e, a.N - 1);
+      w_scale[e] = a.b_scale[at];
+      bias[e] = a.bias ? a.bias[at] : 0.0f;
+    }
+    for (uint32_t r = lane; r < 32 * MI; r += 64) {
+      x_scale[r] = a.a_scale[min(m0 + r, a.M - 1)];
+      big |= x_scale[r] > kBigScale;
+    }
+    big = __any(big);
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<int4v*>(stage + (lane & 31) * kRow + (32 * j + 8 * g + 4 * (lane >> 5)) * 4) =
+            int4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+    wait_loads<63>();   // (the wavefront's writes have arrived)
+#pragma unroll
+    for (uint32_t it = 0; it < 32 / kRows; ++it) {
+      const uint32_t row = it * kRows + lane / kChunks, m = m0 + 32 * i + row;
+      const int4v* from = reinterpret_cast<const int4v*>(stage + row * kRow + lane % kChunks * kPer * 4);
+      uint4 out;
+      if constexpr (TYPE == kSums) {
+        out = __builtin_bit_cast(uint4, from[0]);
+      } else {
+        const float s = x_scale[32 * i + row];
+        float v[kPer];
+#pragma unroll
+        for (uint32_t e = 0; e < kPer; ++e) v[e] = __builtin_fmaf((float)from[e / 4][e % 4] * s, w_scale[e], bias[e]);
+        if (big) {
+#pragma unroll
+          for (uint32_t e = 0; e < kPer; ++e) v[e] = result((float)from[e / 4][e % 4], s, w_scale[e], bias[e]);
+        }
+        if constexpr (kSize == 4) out = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        else out = make_uint4(Element<TYPE>::narrow2(v[0], v[1]), Element<TYPE>::narrow2(v[2], v[3]),
+                              Element<TYPE>::narrow2(v[4], v[5]), Element<TYPE>::narrow2(v[6], v[7]));
+      }
+      if (m >= a.M || n >= a.N) continue;
+      uint8_t* to = TYPE == kSums ? reinterpret_cast<uint8_t*>(a.part) + (((uint64_t)blockIdx.y * a.M + m) * a.N + n) * 4
+                                  : reinterpret_cast<uint8_t*>(a.y) + (m * a.y_ld + n) * kSize;
+      if (n + kPer <= a.N) {
+        using Words = __attribute__((ext_vector_type(4), aligned(kSize))) uint32_t;   // (a row starts anywhere)
+        *reinterpret_cast<Words*>(to) = Words{out.x, out.y, out.z, out.w};
+      } else {
+        const uint32_t w[4] = {out.x, out.y, out.z, out.w};
+#pragma unroll
+        for (uint32_t e = 0; e < kPer; ++e) {
+          if (n + e >= a.N) break;
+          if constexpr (kSize == 4) reinterpret_cast<uint32_t*>(to)[e] = w[e];
+          else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+        }
+      }
+    }
+    wait_loads<63>();   // (... and its reads)
+  }
+}
+
+template <int MI, int NI, int STAGES>
+__global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPair pair) {
   constexpr uint32_t TM = 64 * MI, TN = 64 * NI, kStage = (TM + TN) * kDepth;
   constexpr int kLoads = 2 * (MI + NI);   // of a wavefront and stage, 8 rows each
   __shared__ __attribute__((aligned(16))) uint8_t s0[kStage], s1[kStage], s2[STAGES > 2 ? kStage : 16], s3[STAGES > 3 ? kStage : 16];
+  const bool second = blockIdx.x >= pair.first;   // (of two products: the workgroups behind the first one's)
+  const ProductArgs& a = pair.of[second];
   uint32_t tm, tn;
-  place_tile(blockIdx.x, (a.M + TM - 1) / TM, (a.N + TN - 1) / TN, tm, tn);
+  place_tile(blockIdx.x - (second ? pair.first : 0), (a.M + TM - 1) / TM, (a.N + TN - 1) / TN, tm, tn);
   const uint32_t m0 = tm * TM, n0 = tn * TN;
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t k0 = blockIdx.y * a.split_k, k1 = min(k0 + a.split_k, a.K);
@@ -240,75 +316,13 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductArg
       }
     }
   }
-  // The results leave through LDS, 32 rows of the wavefront's part at a time, so that a store covers whole lines.
   meet();   // (all wavefronts have read their last stage)
-  constexpr uint32_t kSize = TYPE == QSGD_TYPE_F32 || TYPE == kSums ? 4 : 2, kPer = 16 / kSize;   // results of 16 bytes
-  constexpr uint32_t kRow = 32 * NI * 4 + 16, kChunks = 32 * NI / kPer, kRows = 64 / kChunks;      // rows that a store covers
-  static_assert(32 * kRow + 32 * MI * 4 <= kStage / 2, "");
+  // a wavefront's rows of y's tile, written as y's type asks
   uint8_t* stage = (wave < 2 ? s0 : s1) + (wave & 1) * (kStage / 2);
-  float* x_scale = reinterpret_cast<float*>(stage + 32 * kRow);
-  const uint32_t n = n0 + wn + lane % kChunks * kPer;   // a lane's columns are the same for every row
-  float w_scale[kPer], bias[kPer];
-  bool big = false;   // any row's scale is
-  if constexpr (TYPE != kSums) {
-#pragma unroll
-    for (uint32_t e = 0; e < kPer; ++e) {
-      const uint32_t at = min(n + e, a.N - 1);
-      w_scale[e] = a.b_scale[at];
-      bias[e] = a.bias ? a.bias[at] : 0.0f;
-    }
-    for (uint32_t r = lane; r < 32 * MI; r += 64) {
-      x_scale[r] = a.a_scale[min(m0 + wm + r, a.M - 1)];
-      big |= x_scale[r] > kBigScale;
-    }
-    big = __any(big);
-  }
-#pragma unroll
-  for (int i = 0; i < MI; ++i) {
-#pragma unroll
-    for (int j = 0; j < NI; ++j)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<int4v*>(stage + (lane & 31) * kRow + (32 * j + 8 * g + 4 * (lane >> 5)) * 4) =
-            int4v{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-    wait_loads<63>();   // (the wavefront's writes have arrived)
-#pragma unroll
-    for (uint32_t it = 0; it < 32 / kRows; ++it) {
-      const uint32_t row = it * kRows + lane / kChunks, m = m0 + wm + 32 * i + row;
-      const int4v* from = reinterpret_cast<const int4v*>(stage + row * kRow + lane % kChunks * kPer * 4);
-      uint4 out;
-      if constexpr (TYPE == kSums) {
-        out = __builtin_bit_cast(uint4, from[0]);
-      } else {
-        const float s = x_scale[32 * i + row];
-        float v[kPer];
-#pragma unroll
-        for (uint32_t e = 0; e < kPer; ++e) v[e] = __builtin_fmaf((float)from[e / 4][e % 4] * s, w_scale[e], bias[e]);
-        if (big) {
-#pragma unroll
-          for (uint32_t e = 0; e < kPer; ++e) v[e] = result((float)from[e / 4][e % 4], s, w_scale[e], bias[e]);
-        }
-        if constexpr (kSize == 4) out = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        else out = make_uint4(Element<TYPE>::narrow2(v[0], v[1]), Element<TYPE>::narrow2(v[2], v[3]),
-                              Element<TYPE>::narrow2(v[4], v[5]), Element<TYPE>::narrow2(v[6], v[7]));
-      }
-      if (m >= a.M || n >= a.N) continue;
-      uint8_t* to = TYPE == kSums ? reinterpret_cast<uint8_t*>(a.part) + (((uint64_t)blockIdx.y * a.M + m) * a.N + n) * 4
-                                  : reinterpret_cast<uint8_t*>(a.y) + (m * a.y_ld + n) * kSize;
-      if (a.wide && n + kPer <= a.N) {
-        *reinterpret_cast<uint4*>(to) = out;
-      } else {
-        const uint32_t w[4] = {out.x, out.y, out.z, out.w};
-#pragma unroll
-        for (uint32_t e = 0; e < kPer; ++e) {
-          if (n + e >= a.N) break;
-          if constexpr (kSize == 4) reinterpret_cast<uint32_t*>(to)[e] = w[e];
-          else reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
-        }
-      }
-    }
-    wait_loads<63>();   // (... and its reads)
-  }
+  if (a.part) leave<MI, NI, kStage / 2, kSums>(a, acc, stage, m0 + wm, n0 + wn);
+  else if (a.type == QSGD_TYPE_F32) leave<MI, NI, kStage / 2, QSGD_TYPE_F32>(a, acc, stage, m0 + wm, n0 + wn);
+  else if (a.type == QSGD_TYPE_BF16) leave<MI, NI, kStage / 2, QSGD_TYPE_BF16>(a, acc, stage, m0 + wm, n0 + wn);
+  else leave<MI, NI, kStage / 2, QSGD_TYPE_F16>(a, acc, stage, m0 + wm, n0 + wn);
 }
 
 // ---- few rows ---------------------------------------------------------------------
@@ -317,7 +331,7 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductArg
 // operands, so it need not be the matrix instruction's own), straight from memory: no two wavefronts share them.
 constexpr uint32_t kFewDepth = 256;
 
-template <int MT, int NT, uint32_t TYPE>
+template <int MT, int NT>
 __global__ __launch_bounds__(1024) void k_product_few(ProductArgs a) {
   __shared__ __attribute__((aligned(16))) int sums[16][MT * NT * 256];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
@@ -368,13 +382,13 @@ __global__ __launch_bounds__(1024) void k_product_few(ProductArgs a) {
     if (m >= a.M || n >= a.N) continue;
     int sum = 0;
     for (uint32_t s = 0; s < waves; ++s) sum += sums[s][o];
-    if constexpr (TYPE == kSums) a.part[((uint64_t)blockIdx.y * a.M + m) * a.N + n] = sum;
-    else put<TYPE>(a, m, n, (float)sum);
+    if (a.part) a.part[((uint64_t)blockIdx.y * a.M + m) * a.N + n] = sum;
+    else put(a, m, n, (float)sum);
   }
 }
 
 // The pieces' sums, added in 64 bits: PER neighbouring results of a row to a thread.
-template <uint32_t TYPE, int PER>
+template <int PER>
 __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
   const uint64_t all = (uint64_t)a.M * a.N, i = PER * ((uint64_t)blockIdx.x * 256 + threadIdx.x);
   if (i >= all) return;
@@ -388,7 +402,7 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
   }
   const uint32_t m = all >> 32 ? (uint32_t)(i / a.N) : (uint32_t)i / a.N, n = (uint32_t)(i - (uint64_t)m * a.N);
 #pragma unroll
-  for (int e = 0; e < PER; ++e) put<TYPE>(a, m, n + e, (float)sum[e]);
+  for (int e = 0; e < PER; ++e) put(a, m, n + e, (float)sum[e]);
 }
 
 }  // namespace
@@ -437,45 +451,32 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
   return best;
 }
 
-namespace {
-
-template <uint32_t TYPE>
-void launch_as(const ProductArgs& a, uint32_t kind, hipStream_t st) {
+hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t st) {
+  const ProductArgs& a = pair.of[0];
   auto tiles = [&](auto kernel, uint32_t size) {
-    const dim3 grid((a.M + size - 1) / size * ((a.N + size - 1) / size), a.splits);
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
+    ProductPair p = pair;
+    auto count = [&](const ProductArgs& x) { return (x.M + size - 1) / size * ((x.N + size - 1) / size); };
+    p.first = count(a);
+    const dim3 grid(p.first + (pair.count > 1 ? count(pair.of[1]) : 0), a.splits);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, p);
   };
   if (kind == kProductFew) {
     const uint32_t steps = (std::min(a.K, a.split_k) + kFewDepth - 1) / kFewDepth;
-    const dim3 block(64 * std::max(1u, std::min(steps, 16u)));
-    if (a.M <= 16) hipLaunchKernelGGL((k_product_few<1, 1, TYPE>), dim3((a.N + 15) / 16, a.splits), block, 0, st, a);
-    else hipLaunchKernelGGL((k_product_few<2, 1, TYPE>), dim3((a.N + 15) / 16, a.splits), block, 0, st, a);
+    const dim3 block(64 * std::max(1u, std::min(steps, 16u))), grid((a.N + 15) / 16, a.splits);
+    if (a.M <= 16) hipLaunchKernelGGL((k_product_few<1, 1>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_product_few<2, 1>), grid, block, 0, st, a);
   }
-  else if (kind == kProductTile64Deep) tiles(k_product<1, 1, 4, TYPE>, 64);
-  else if (kind == kProductTile64) tiles(k_product<1, 1, 2, TYPE>, 64);
-  else if (kind == kProductTile128) tiles(k_product<2, 2, 2, TYPE>, 128);
-  else tiles(k_product<4, 4, 2, TYPE>, 256);
-}
-
-}  // namespace
-
-hipError_t launch_product(const ProductArgs& a, uint32_t kind, hipStream_t st) {
-  if (a.part) launch_as<kSums>(a, kind, st);
-  else if (a.type == QSGD_TYPE_F32) launch_as<QSGD_TYPE_F32>(a, kind, st);
-  else if (a.type == QSGD_TYPE_BF16) launch_as<QSGD_TYPE_BF16>(a, kind, st);
-  else launch_as<QSGD_TYPE_F16>(a, kind, st);
+  else if (kind == kProductTile64Deep) tiles(k_product<1, 1, 4>, 64);
+  else if (kind == kProductTile64) tiles(k_product<1, 1, 2>, 64);
+  else if (kind == kProductTile128) tiles(k_product<2, 2, 2>, 128);
+  else tiles(k_product<4, 4, 2>, 256);
   return hipGetLastError();
 }
 
 hipError_t launch_product_join(const ProductArgs& a, hipStream_t st) {
   const uint64_t all = (uint64_t)a.M * a.N;
-  auto go = [&](auto four, auto one) {
-    if (a.N % 4 == 0) hipLaunchKernelGGL(four, dim3((uint32_t)((all / 4 + 255) / 256)), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(one, dim3((uint32_t)((all + 255) / 256)), dim3(256), 0, st, a);
-  };
-  if (a.type == QSGD_TYPE_F32) go(k_product_join<QSGD_TYPE_F32, 4>, k_product_join<QSGD_TYPE_F32, 1>);
-  else if (a.type == QSGD_TYPE_BF16) go(k_product_join<QSGD_TYPE_BF16, 4>, k_product_join<QSGD_TYPE_BF16, 1>);
-  else go(k_product_join<QSGD_TYPE_F16, 4>, k_product_join<QSGD_TYPE_F16, 1>);
+  if (a.N % 4 == 0) hipLaunchKernelGGL(k_product_join<4>, dim3((uint32_t)((all / 4 + 255) / 256)), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_product_join<1>, dim3((uint32_t)((all + 255) / 256)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -184,38 +184,37 @@ __device__ __forceinline__ void columns_block(const QuantizeArgs& a, uint32_t bl
       take(x);
     }
   }
-  // the parts' results, joined by halves
-  float* const sum = reinterpret_cast<float*>(shared + 256 * 8);
-  auto at = [&](uint32_t t, int i) { return 256 * i + t; };
-  uint32_t m[8];
+  // the parts' results: eight of them to a thread, then what is left to one per column
+  const uint32_t width = 8 * lanes;
+  uint32_t* const most_of = shared;
+  float* const sum_of = reinterpret_cast<float*>(shared + 256 * 8);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    m[i] = most.column(i);
-    shared[at(threadIdx.x, i)] = m[i];
-    if (sums) sum[at(threadIdx.x, i)] = s[i];
+    most_of[width * part + 8 * lane + i] = most.column(i);
+    if (sums) sum_of[width * part + 8 * lane + i] = s[i];
   }
-  for (uint32_t half = 128; half >= lanes; half >>= 1) {
-    __syncthreads();
-    if (threadIdx.x < half) {
+  __syncthreads();
+  const uint32_t col = threadIdx.x % width, piece = threadIdx.x / width;
+  uint32_t m = 0;
+  float sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        m[i] = max(m[i], shared[at(threadIdx.x + half, i)]);
-        shared[at(threadIdx.x, i)] = m[i];
-        if (sums) {
-          s[i] += sum[at(threadIdx.x + half, i)];
-          sum[at(threadIdx.x, i)] = s[i];
-        }
-      }
-    }
+  for (uint32_t i = 0; i < 8; ++i) {
+    m = max(m, most_of[width * (8 * piece + i) + col]);
+    if (sums) sum += sum_of[width * (8 * piece + i) + col];
   }
-  if (threadIdx.x < lanes) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (c + i >= a.cols) break;
-      const uint64_t to = (uint64_t)chunk * a.cols + c + i;
-      if (a.part_max) a.part_max[to] = m[i];
-      if (sums) a.part_sum[to] = s[i];
+  __syncthreads();
+  most_of[threadIdx.x] = m;
+  if (sums) sum_of[threadIdx.x] = sum;
+  __syncthreads();
+  const uint32_t to_c = width * strip + threadIdx.x;
+  if (threadIdx.x < width && to_c < a.cols) {
+    for (uint32_t i = 1; i < 256 / width; ++i) {
+      m = max(m, most_of[width * i + threadIdx.x]);
+      if (sums) sum += sum_of[width * i + threadIdx.x];
     }
+    const uint64_t to = (uint64_t)chunk * a.cols + to_c;
+    if (a.part_max) a.part_max[to] = m;
+    if (sums) a.part_sum[to] = sum;
   }
 }
 
@@ -247,16 +246,46 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
   while (block >= jobs.job[j].tile_blocks) block -= jobs.job[j++].tile_blocks;   // (the grid is their sum)
   const QuantizeArgs& a = jobs.job[j];
   const uint32_t strips = (a.cols + 63) / 64, c0 = block % strips * 64, first = block / strips * a.tile_rows;
+  const uint32_t cx = threadIdx.x & 7, ry = threadIdx.x >> 3, c = c0 + 8 * cx;
+  const uint32_t iteration = STOCHASTIC ? draw_iteration(a.draws) : 0;
+  const uint32_t end = min(first + a.tile_rows, a.rows);
+  Eight<TYPE> x[4];
+  HalfWords h[4];
+  auto load = [&](uint32_t r) {   // four rows' eight columns, and their draws
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = {};
+      if (c < a.cols && r + i < end) {
+        const void* p = element_at<TYPE>(a.x, a.ld, r + i, c);
+        if (a.stream) x[i].template load<true>(p, a.cols - c);
+        else x[i].load(p, a.cols - c);
+      }
+    }
+    if constexpr (STOCHASTIC) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = draw_block(a.draws, iteration, r + i, c / 8);
+    }
+  };
+  if (a.part_max) load(first + 4 * ry);
   {   // the chunks' maxima and sums, by four threads to a column
-    const uint32_t c = c0 + (threadIdx.x & 63), part = threadIdx.x >> 6;
+    const uint32_t column = c0 + (threadIdx.x & 63), part = threadIdx.x >> 6;
     uint32_t m = 0;
     float s = 0.0f;
     const bool sums = a.part_sum && first == 0;
-    if (c < a.cols) {
-      for (uint32_t k = part; k < a.chunks; k += 4) {
-        const uint64_t at = (uint64_t)k * a.cols + c;
-        if (a.part_max) m = max(m, a.part_max[at]);
-        if (sums) s += a.part_sum[at];
+    if (column < a.cols) {
+      for (uint32_t k = part; k < a.chunks; k += 16) {   // (four on their way)
+        uint32_t v[4] = {};
+        float w[4] = {};
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+          const uint64_t at = (uint64_t)(k + 4 * i) * a.cols + column;
+          if (k + 4 * i < a.chunks) {
+            if (a.part_max) v[i] = a.part_max[at];
+            if (sums) w[i] = a.part_sum[at];
+          }
+        }
+        m = max(m, max(max(v[0], v[1]), max(v[2], v[3])));
+        s += (w[0] + w[1]) + (w[2] + w[3]);
       }
     }
     found[part][threadIdx.x & 63] = m;
@@ -268,50 +297,32 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
       float scale, inv;
       scale_of(__uint_as_float(m), scale, inv);
       factor[t] = inv;
-      if (first == 0 && c < a.cols) {
-        if (a.part_max) a.col_scale[c] = scale;
-        if (sums) a.col_sum[c] = (added[0][t] + added[1][t]) + (added[2][t] + added[3][t]);
+      if (first == 0 && column < a.cols) {
+        if (a.part_max) a.col_scale[column] = scale;
+        if (sums) a.col_sum[column] = (added[0][t] + added[1][t]) + (added[2][t] + added[3][t]);
       }
     }
     __syncthreads();
   }
   if (!a.part_max) return;
-  const uint32_t cx = threadIdx.x & 7, ry = threadIdx.x >> 3, c = c0 + 8 * cx;
-  const uint32_t iteration = STOCHASTIC ? draw_iteration(a.draws) : 0;
   float inv[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) inv[i] = factor[8 * cx + i];
-  const uint32_t end = min(first + a.tile_rows, a.rows);
   // word w of column n: the 16-byte places of a column change with its number, so that eight threads' words do not meet
   auto at = [&](uint32_t n, uint32_t w) { return 32 * n + 4 * ((w >> 2) ^ (n >> 3 & 7)) + (w & 3); };
   for (uint32_t r0 = first; r0 < end; r0 += 128) {
-    const uint32_t r = r0 + 4 * ry;
-    if (c < a.cols && r < a.rows) {
-      Eight<TYPE> x[4] = {};
-      HalfWords h[4] = {};
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (r + i < a.rows) {
-          const void* p = element_at<TYPE>(a.x, a.ld, r + i, c);
-          if (a.stream) x[i].template load<true>(p, a.cols - c);
-          else x[i].load(p, a.cols - c);
-        }
-      if constexpr (STOCHASTIC) {
+    for (int n = 0; n < 8; ++n) {
+      float t[4];
+      uint32_t left[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = draw_block(a.draws, iteration, r + i, c / 8);
+      for (int i = 0; i < 4; ++i) {
+        t[i] = x[i].value(n) * inv[n];
+        left[i] = STOCHASTIC ? draw_left(h[i], n) : 0;
       }
-#pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        float t[4];
-        uint32_t left[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          t[i] = x[i].value(n) * inv[n];
-          left[i] = draw_left(h[i], n);
-        }
-        tile[at(8 * cx + n, ry)] = STOCHASTIC ? stochastic_levels(t, left) : nearest_levels(t);
-      }
+      tile[at(8 * cx + n, ry)] = STOCHASTIC ? stochastic_levels(t, left) : nearest_levels(t);
     }
+    if (r0 + 128 < end) load(r0 + 128 + 4 * ry);
     __syncthreads();
 #pragma unroll
     for (uint32_t p = 0; p < 2; ++p) {
@@ -339,10 +350,10 @@ void plan_columns(uint32_t rows, uint32_t cols, uint32_t& strip_lanes, uint32_t&
   strip_lanes = 16;
   while (strip_lanes > 1 && 4 * strip_lanes >= cols) strip_lanes /= 2;   // narrow matrices: more rows side by side
   const uint64_t strips = (cols + 8ull * strip_lanes - 1) / (8 * strip_lanes);
-  // about 1024 workgroups, 64 chunks at most (each is read again by every tile of the second launch), and eight rows
+  // about 1024 workgroups, 64 chunks at most (each is read again by every tile of the second launch), and four rows
   // at least to every thread
   const uint64_t want = strips ? (1024 + strips - 1) / strips : 1;
-  const uint64_t least = 8ull * (256 / strip_lanes);
+  const uint64_t least = 4ull * (256 / strip_lanes);
   const uint64_t each = (rows + (want < 64 ? want : 64) - 1) / (want < 64 ? want : 64);
   chunk_rows = (uint32_t)(each < least ? least : each);
   chunks = (rows + chunk_rows - 1) / chunk_rows;
