@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libqsgd.so")
 SOURCES = ["qsgd_capi.hip", "qsgd_encode.hip", "qsgd_encode_direct.hip", "qsgd_decode.hip", "qsgd_decode_tile.hip",
            "qsgd_decode_split.hip", "qsgd_general.hip", "qsgd_tensors.hip", "qsgd_pipeline.hip",
            "qsgd_layer.hip", "qsgd_dropout.hip", "qsgd_quantize.hip", "qsgd_product.hip"]
-HEADERS = ["qsgd_device.hpp", "qsgd_kernels.hpp", "qsgd_encode_wave.hpp", "qsgd_layer.hpp"]
+HEADERS = ["qsgd_device.hpp", "qsgd_kernels.hpp", "qsgd_encode_wave.hpp", "qsgd_layer.hpp", "qsgd_levels.hpp"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

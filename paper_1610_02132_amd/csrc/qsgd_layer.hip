@@ -301,17 +301,22 @@ int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_m
   if (!room(workspace_dev, workspace_bytes, s.bytes)) return no_room(workspace_dev, s.bytes);
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   uint8_t* ws = reinterpret_cast<uint8_t*>(workspace_dev);
+  ProductArgs p = {};
+  p.b = reinterpret_cast<const int8_t*>(w->data_dev); p.b_ld = w->ld;
+  p.M = (uint32_t)x->rows; p.N = (uint32_t)w->rows; p.K = (uint32_t)x->cols;
+  p.b_scale = w_scale_dev; p.bias = bias_dev;
+  p.y = y->data_dev; p.y_ld = y->ld; p.type = y->type;
+  if (linear_few_fits(p.M, p.N, p.K)) {
+    ScopedTiming tm("linear_few", st);
+    return status(launch_linear_few({p, x->data_dev, x->ld, d}, x->type, rounding == QSGD_ROUND_STOCHASTIC, st));
+  }
   const uint64_t ld = levels_ld(x->cols);
   QuantizeJobs jobs = {1, {job(x, d)}};
   QuantizeArgs& q = jobs.job[0];
   want_rows(q, reinterpret_cast<int8_t*>(ws), ld, reinterpret_cast<float*>(ws + s.scale));
   if (int rc = quantize(jobs, x->type, rounding, st)) return rc;
-  ProductArgs p = {};
   p.a = q.q_rows; p.a_ld = ld;
-  p.b = reinterpret_cast<const int8_t*>(w->data_dev); p.b_ld = w->ld;
-  p.M = (uint32_t)x->rows; p.N = (uint32_t)w->rows; p.K = (uint32_t)x->cols;
-  p.a_scale = q.row_scale; p.b_scale = w_scale_dev; p.bias = bias_dev;
-  p.y = y->data_dev; p.y_ld = y->ld; p.type = y->type;
+  p.a_scale = q.row_scale;
   return product(p, s.plan, ws + s.rest, st);
 }
 

@@ -32,6 +32,20 @@ __device__ __forceinline__ HalfWords draw_block(const DrawArgs& d, uint32_t iter
   return h;
 }
 
+// Several blocks at once: the key is stepped once for all of them, and products of words that they share are made once.
+template <int N>
+__device__ __forceinline__ void draw_blocks(const DrawArgs& d, uint32_t iteration, const uint32_t (&row)[N],
+                                            const uint32_t (&c8)[N], HalfWords* h) {
+  uint32_t c1[N], out[N][4];
+#pragma unroll
+  for (int i = 0; i < N; ++i) c1[i] = d.row_base + row[i];
+  philox4x32_10_xn<N>(c8, c1, d.stream_id, iteration, d.key0, d.key1, out);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) h[i].w[j] = out[i][j];
+}
+
 // ---- element types ---------------------------------------------------------------
 // A value's bits, their fp32 value, and fp32 rounded to the type (nearest, ties to even).
 template <uint32_t TYPE> struct Element;
@@ -178,6 +192,15 @@ struct ProductPlan { uint32_t kind, splits, split_k; uint64_t bytes; };
 struct ProductPair { ProductArgs of[2]; uint32_t count, first; };
 ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K);
 hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t st);
+// The layer on few tokens, x quantized on the way: product has no a and no a_scale.
+struct LinearArgs {
+  ProductArgs product;
+  const void* x;
+  uint64_t x_ld;
+  DrawArgs draws;
+};
+bool linear_few_fits(uint32_t M, uint32_t N, uint32_t K);
+hipError_t launch_linear_few(const LinearArgs& l, uint32_t type, bool stochastic, hipStream_t st);
 hipError_t launch_product_join(const ProductArgs& a, hipStream_t st);
 
 }  // namespace qsgd

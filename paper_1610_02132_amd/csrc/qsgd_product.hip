@@ -6,6 +6,7 @@
 #include <cmath>
 
 #include "qsgd_layer.hpp"
+#include "qsgd_levels.hpp"
 
 namespace qsgd {
 namespace {
@@ -25,8 +26,8 @@ __device__ __forceinline__ float result(float sum, float s, float t, float bias)
   return s > kBigScale ? sum * (s * 0x1p-64f) * t * 0x1p64f + bias : __builtin_fmaf(sum * s, t, bias);
 }
 
-__device__ __forceinline__ void put(const ProductArgs& a, uint32_t m, uint32_t n, float sum) {
-  const float v = result(sum, a.a_scale[m], a.b_scale[n], a.bias ? a.bias[n] : 0.0f);
+__device__ __forceinline__ void put(const ProductArgs& a, uint32_t m, uint32_t n, float sum, float row_scale) {
+  const float v = result(sum, row_scale, a.b_scale[n], a.bias ? a.bias[n] : 0.0f);
   const uint64_t at = m * a.y_ld + n;
   if (a.type == QSGD_TYPE_F32) reinterpret_cast<float*>(a.y)[at] = v;
   else reinterpret_cast<uint16_t*>(a.y)[at] = (uint16_t)(a.type == QSGD_TYPE_BF16 ? Element<QSGD_TYPE_BF16>::narrow(v) : Element<QSGD_TYPE_F16>::narrow(v));
@@ -383,7 +384,83 @@ __global__ __launch_bounds__(1024) void k_product_few(ProductArgs a) {
     int sum = 0;
     for (uint32_t s = 0; s < waves; ++s) sum += sums[s][o];
     if (a.part) a.part[((uint64_t)blockIdx.y * a.M + m) * a.N + n] = sum;
-    else put(a, m, n, (float)sum);
+    else put(a, m, n, (float)sum, a.a_scale[m]);
+  }
+}
+
+// The layer for few tokens, their quantizing included: every workgroup makes the levels of all of them (in LDS, where
+// its wavefronts' turns find them) while the weights of its first turn are on their way, which costs less than a launch.
+template <uint32_t TYPE, bool STOCHASTIC>
+__global__ __launch_bounds__(1024) void k_linear_few(LinearArgs l) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  __shared__ uint32_t most[16];
+  __shared__ float scale[16], factor[16];
+  const ProductArgs& a = l.product;
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  int* const sums = reinterpret_cast<int*>(lds);                       // 256 for each wavefront
+  uint8_t* const levels = lds + 1024 * waves;                          // rows of `stride`, zeros behind K
+  const uint32_t n0 = blockIdx.x * 16, own = 64 * (lane >> 4), whole = (a.K + kFewDepth - 1) / kFewDepth * kFewDepth;
+  const uint32_t stride = whole + 16;
+  int4v w[4];
+  auto weights = [&](uint32_t k) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = operand(a.b, a.b_ld, n0 + (lane & 15), a.N, k + own + 16 * j, a.K);
+  };
+  weights(wave * kFewDepth);
+  // a row to `parts` wavefronts, or several rows to one
+  const uint32_t parts = waves > a.M ? waves / a.M : 1, part = wave / a.M, step = waves > a.M ? a.M : waves;
+  const uint32_t row0 = part < parts ? wave % a.M : a.M, c8s = (a.K + 7) / 8;
+  if (threadIdx.x < 16) most[threadIdx.x] = 0;
+  __syncthreads();
+  for (uint32_t m = row0; m < a.M; m += step) {
+    Largest<TYPE> largest;
+    for (uint32_t c8 = 64 * part + lane; c8 < c8s; c8 += 64 * parts) {
+      Eight<TYPE> x;
+      x.load(element_at<TYPE>(l.x, l.x_ld, m, 8 * c8), a.K - 8 * c8);
+      largest.add(x);
+    }
+    uint32_t v = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v = max(v, largest.column(i));
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+    if (lane == 0) atomicMax(&most[m], v);
+  }
+  __syncthreads();
+  if (threadIdx.x < a.M) scale_of(__uint_as_float(most[threadIdx.x]), scale[threadIdx.x], factor[threadIdx.x]);
+  __syncthreads();
+  const uint32_t iteration = STOCHASTIC ? draw_iteration(l.draws) : 0;
+  for (uint32_t m = row0; m < a.M; m += step) {
+    const float inv = factor[m];
+    for (uint32_t c8 = 64 * part + lane; c8 < whole / 8; c8 += 64 * parts) {
+      uint32_t q[2] = {0, 0};
+      if (c8 < c8s) {
+        Eight<TYPE> x;
+        x.load(element_at<TYPE>(l.x, l.x_ld, m, 8 * c8), a.K - 8 * c8);
+        HalfWords h = {};
+        if constexpr (STOCHASTIC) h = draw_block(l.draws, iteration, m, c8);
+        eight_levels<TYPE, STOCHASTIC>(x, inv, h, q);
+      }
+      *reinterpret_cast<uint2*>(levels + m * stride + 8 * c8) = make_uint2(q[0], q[1]);
+    }
+  }
+  __syncthreads();
+  int4v acc = {};
+  for (uint32_t k = wave * kFewDepth; k < a.K; k += waves * kFewDepth) {
+    if (k >= waves * kFewDepth) weights(k);
+    const int4v* x = reinterpret_cast<const int4v*>(levels + min(lane & 15, a.M - 1) * stride + k + own);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], x[j], acc, 0, 0, 0);
+  }
+  *reinterpret_cast<int4v*>(&sums[256 * wave + (lane & 15) * 16 + 4 * (lane >> 4)]) = acc;
+  __syncthreads();
+  if (threadIdx.x < 256) {
+    const uint32_t m = threadIdx.x / 16, n = n0 + threadIdx.x % 16;
+    if (m < a.M && n < a.N) {
+      int sum = 0;
+      for (uint32_t s = 0; s < waves; ++s) sum += sums[256 * s + threadIdx.x];
+      put(a, m, n, (float)sum, scale[m]);
+    }
   }
 }
 
@@ -402,7 +479,7 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
   }
   const uint32_t m = all >> 32 ? (uint32_t)(i / a.N) : (uint32_t)i / a.N, n = (uint32_t)(i - (uint64_t)m * a.N);
 #pragma unroll
-  for (int e = 0; e < PER; ++e) put(a, m, n + e, (float)sum[e]);
+  for (int e = 0; e < PER; ++e) put(a, m, n + e, (float)sum[e], a.a_scale[m]);
 }
 
 }  // namespace
@@ -470,6 +547,25 @@ hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t s
   else if (kind == kProductTile64) tiles(k_product<1, 1, 2>, 64);
   else if (kind == kProductTile128) tiles(k_product<2, 2, 2>, 128);
   else tiles(k_product<4, 4, 2>, 256);
+  return hipGetLastError();
+}
+
+// Whether quantizing in every workgroup is the faster way: not where many of them make many levels each, or where the
+// weights have so many rows that the tile kernels read them faster (us, together and apart, bf16, M x N x K: 1 x 4096 x 4096
+// 7.6 / 10.5, 8 x 4096 x 4096 9.6 / 10.6, 1 x 8192 x 8192 15.3 / 18.1, 1 x 16384 x 4096 18.2 / 16.8, 16 x 8192 x 2048 12.1 / 10.6).
+// LDS holds 16 KiB of sums and 47 KiB of levels.
+bool linear_few_fits(uint32_t M, uint32_t N, uint32_t K) {
+  return M <= 16 && N <= 8192 && K > 0 && (uint64_t)M * (K + 272) <= 47u << 10 && (uint64_t)M * K * ((N + 15) / 16) <= 12u << 20;
+}
+
+hipError_t launch_linear_few(const LinearArgs& l, uint32_t type, bool stochastic, hipStream_t st) {
+  const ProductArgs& a = l.product;
+  const uint32_t steps = (a.K + kFewDepth - 1) / kFewDepth, waves = std::max(4u, std::min(steps, 16u));
+  const uint32_t lds = 1024 * waves + a.M * (steps * kFewDepth + 16);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((a.N + 15) / 16), dim3(64 * waves), lds, st, l); };
+  if (type == QSGD_TYPE_F32) stochastic ? go(k_linear_few<QSGD_TYPE_F32, true>) : go(k_linear_few<QSGD_TYPE_F32, false>);
+  else if (type == QSGD_TYPE_BF16) stochastic ? go(k_linear_few<QSGD_TYPE_BF16, true>) : go(k_linear_few<QSGD_TYPE_BF16, false>);
+  else stochastic ? go(k_linear_few<QSGD_TYPE_F16, true>) : go(k_linear_few<QSGD_TYPE_F16, false>);
   return hipGetLastError();
 }
 

@@ -4,86 +4,18 @@
 // Memory bound: the row form reads a row once, the column form reads the matrix twice (a column does not fit
 // a compute unit).
 #include "qsgd_layer.hpp"
+#include "qsgd_levels.hpp"
 
 namespace qsgd {
 namespace {
-
-// Largest magnitude -> scale and the factor fl(127 / m); zero rows get zeros, rows with an infinity or a NaN
-// the scale NaN and the factor 0.
-__device__ __forceinline__ void scale_of(float m, float& scale, float& inv) {
-  const bool finite = m < __builtin_huge_valf(), tiny = m < kTinyMax;
-  inv = finite && !tiny ? 127.0f / m : 0.0f;
-  scale = !finite ? __builtin_nanf("") : tiny ? 0.0f : m / 127.0f;
-}
-
-// Four words' bytes of one number in a word.
-template <int BYTE>
-__device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0C0C0400u | BYTE << 8 | BYTE);
-  const uint32_t hi = __builtin_amdgcn_perm(d, c, 0x04000C0Cu | (uint32_t)BYTE << 24 | (uint32_t)BYTE << 16);
-  return lo | hi;
-}
-
-// The levels of four values t (scaled to 127) as signed bytes of a word.  An infinity or a NaN in t (inv is 0 then, or the
-// value itself) becomes level 0: the conversions to whole numbers say 0 for a NaN, and 0 times an infinity is one.
-__device__ __forceinline__ uint32_t nearest_levels(const float (&t)[4]) {
-  int q[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) q[i] = (int)__builtin_rintf(t[i]);
-  return pack_bytes<0>(q[0], q[1], q[2], q[3]);
-}
-
-// Up iff (h + 1/2) / 65536 is below the fraction of |t|:  with R = ceil(65536 |t| - 1/2), a whole number that fp32
-// holds exactly (|t| <= 127 + 2^-17, the next number after 127, so that R <= 127 * 65536 and no level passes 127),
-// the level is the upper half of R + 65535 - h.  `left` has 65535 - h.
-__device__ __forceinline__ uint32_t stochastic_levels(const float (&t)[4], const uint32_t (&left)[4]) {
-  uint32_t q[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    q[i] = (uint32_t)__builtin_ceilf(__builtin_fmaf(fabsf(t[i]), 65536.0f, -0.5f)) + left[i];
-  const uint32_t level = pack_bytes<2>(q[0], q[1], q[2], q[3]);
-  // a byte of ones where t is negative, and the negative of those bytes: no carry leaves bit 7, which is put in last
-  const uint32_t minus = __builtin_amdgcn_perm(__float_as_uint(t[1]), __float_as_uint(t[0]), 0x0C0C0B09u) |
-                         __builtin_amdgcn_perm(__float_as_uint(t[3]), __float_as_uint(t[2]), 0x0B090C0Cu);
-  const uint32_t flipped = level ^ minus;
-  return ((flipped & 0x7F7F7F7Fu) + (minus & 0x01010101u)) ^ (flipped & 0x80808080u);
-}
-
-// 65535 - h for the draws of column i of a block.
-__device__ __forceinline__ uint32_t draw_left(const HalfWords& h, int i) { return 0xFFFFu - half_word(h, i); }
-
-// Magnitudes' bits, whose order is that of the magnitudes with a NaN above infinity: eight columns, two to a word for
-// 16-bit types.
-template <uint32_t TYPE> struct Largest {
-  static constexpr int kWords = Eight<TYPE>::kWords;
-  uint32_t w[kWords] = {};
-  __device__ __forceinline__ void add(const Eight<TYPE>& x) {
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-      if constexpr (kWords == 8) {
-        w[i] = max(w[i], x.w[i] & 0x7FFFFFFFu);
-      } else {
-        using pair = __attribute__((ext_vector_type(2))) uint16_t;
-        w[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(pair, w[i]),
-                                                                      __builtin_bit_cast(pair, x.w[i] & 0x7FFF7FFFu)));
-      }
-    }
-  }
-  // ... as bits of fp32
-  __device__ __forceinline__ uint32_t column(int i) const {
-    Eight<TYPE> e;
-#pragma unroll
-    for (int j = 0; j < kWords; ++j) e.w[j] = w[j];
-    return __float_as_uint(e.value(i));
-  }
-};
 
 constexpr int kHeld = 4;   // blocks of eight columns of a row that a lane holds in registers
 
 // Rows `first` and following, one to 256 / LANES of the workgroup's parts.
 template <uint32_t TYPE, bool STOCHASTIC, int LANES>
 __device__ __forceinline__ void rows_block(const QuantizeArgs& a, uint32_t first, uint32_t* shared) {
-  const uint32_t lane = threadIdx.x % LANES, r = first + threadIdx.x / LANES, c8s = (a.cols + 7) / 8;
+  // (the row is one for a wavefront, which the compiler is told)
+  const uint32_t lane = threadIdx.x % LANES, r = __builtin_amdgcn_readfirstlane(first + threadIdx.x / LANES), c8s = (a.cols + 7) / 8;
   const bool have = r < a.rows;
   Eight<TYPE> held[kHeld];
   Largest<TYPE> most;
@@ -100,6 +32,13 @@ __device__ __forceinline__ void rows_block(const QuantizeArgs& a, uint32_t first
     x.load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8);
     most.add(x);
   }
+  HalfWords draws[kHeld] = {};   // of the blocks held, while these are on their way
+  const uint32_t iteration = STOCHASTIC ? draw_iteration(a.draws) : 0;
+  if constexpr (STOCHASTIC) {
+    static_assert(kHeld == 4, "");
+    draw_blocks<2>(a.draws, iteration, {r, r}, {lane, LANES + lane}, draws);
+    if (c8s > 2 * LANES) draw_blocks<2>(a.draws, iteration, {r, r}, {2 * LANES + lane, 3 * LANES + lane}, draws + 2);
+  }
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, most.column(i));
@@ -114,22 +53,9 @@ __device__ __forceinline__ void rows_block(const QuantizeArgs& a, uint32_t first
   float scale, inv;
   scale_of(__uint_as_float(m), scale, inv);
   if (lane == 0) a.row_scale[r] = scale;
-  const uint32_t iteration = STOCHASTIC ? draw_iteration(a.draws) : 0;
-  auto put = [&](const Eight<TYPE>& x, uint32_t c8) {
-    HalfWords h = {};
-    if constexpr (STOCHASTIC) h = draw_block(a.draws, iteration, r, c8);
+  auto put = [&](const Eight<TYPE>& x, uint32_t c8, const HalfWords& h) {
     uint32_t q[2];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      float t[4];
-      uint32_t left[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        t[i] = x.value(4 * half + i) * inv;
-        left[i] = draw_left(h, 4 * half + i);
-      }
-      q[half] = STOCHASTIC ? stochastic_levels(t, left) : nearest_levels(t);
-    }
+    eight_levels<TYPE, STOCHASTIC>(x, inv, h, q);
     int8_t* out = a.q_rows + (r * a.q_rows_ld + 8 * c8);
     const uint32_t n = a.cols - 8 * c8;
     if (n >= 8) {
@@ -143,12 +69,14 @@ __device__ __forceinline__ void rows_block(const QuantizeArgs& a, uint32_t first
 #pragma unroll
   for (int u = 0; u < kHeld; ++u) {
     const uint32_t c8 = u * LANES + lane;
-    if (c8 < c8s) put(held[u], c8);
+    if (c8 < c8s) put(held[u], c8, draws[u]);
   }
   for (uint32_t c8 = kHeld * LANES + lane; c8 < c8s; c8 += LANES) {
     Eight<TYPE> x;
     x.load(element_at<TYPE>(a.x, a.ld, r, 8 * c8), a.cols - 8 * c8);
-    put(x, c8);
+    HalfWords h = {};
+    if constexpr (STOCHASTIC) h = draw_block(a.draws, iteration, r, c8);
+    put(x, c8, h);
   }
 }
 
@@ -254,17 +182,15 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
   auto load = [&](uint32_t r) {   // four rows' eight columns, and their draws
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[i] = {};
       if (c < a.cols && r + i < end) {
         const void* p = element_at<TYPE>(a.x, a.ld, r + i, c);
         if (a.stream) x[i].template load<true>(p, a.cols - c);
         else x[i].load(p, a.cols - c);
+      } else {
+        x[i] = {};
       }
     }
-    if constexpr (STOCHASTIC) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = draw_block(a.draws, iteration, r + i, c / 8);
-    }
+    if constexpr (STOCHASTIC) draw_blocks<4>(a.draws, iteration, {r, r + 1, r + 2, r + 3}, {c / 8, c / 8, c / 8, c / 8}, h);
   };
   if (a.part_max) load(first + 4 * ry);
   {   // the chunks' maxima and sums, by four threads to a column
@@ -350,9 +276,9 @@ void plan_columns(uint32_t rows, uint32_t cols, uint32_t& strip_lanes, uint32_t&
   strip_lanes = 16;
   while (strip_lanes > 1 && 4 * strip_lanes >= cols) strip_lanes /= 2;   // narrow matrices: more rows side by side
   const uint64_t strips = (cols + 8ull * strip_lanes - 1) / (8 * strip_lanes);
-  // about 1024 workgroups, 64 chunks at most (each is read again by every tile of the second launch), and four rows
+  // about 512 workgroups, 64 chunks at most (each is read again by every tile of the second launch), and four rows
   // at least to every thread
-  const uint64_t want = strips ? (1024 + strips - 1) / strips : 1;
+  const uint64_t want = strips ? (512 + strips - 1) / strips : 1;
   const uint64_t least = 4ull * (256 / strip_lanes);
   const uint64_t each = (rows + (want < 64 ? want : 64) - 1) / (want < 64 ? want : 64);
   chunk_rows = (uint32_t)(each < least ? least : each);
