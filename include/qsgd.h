@@ -241,6 +241,12 @@ int qsgd_pipeline_step(qsgd_pipeline *pl, const qsgd_params *p, uint64_t chunk_e
  * row or a column of a matrix; the product of two such matrices in integers; a linear layer
  * made of them with its gradients; and dropout from the same counter-based generator.
  * All draws are reproducible from their key and position, no mask or generator state is stored.
+ *
+ * The calls queue kernels on hip_stream on the current device, whose memory the arguments are in, allocate
+ * nothing and may be captured.  An output or a workspace must not overlap another argument, except where said;
+ * outputs that do are refused with QSGD_ERR_INVALID_ARG (column ranges of one larger matrix do not
+ * overlap).  QSGD_ERR_UNSUPPORTED: more work than a launch can count (2^32 blocks of eight columns of dropout,
+ * 2^24 rows of more than 2048 columns of the quantizer, 2^26 rows of an operand, 2^38 results of a product).
  */
 
 /* Element types of a matrix. */

@@ -81,8 +81,10 @@ class Draws:
         t = self.iteration_dev
         if t is None:
             return _pack_draws(self.seed, self.stream_id, self.iteration, self.row_base, 0, 0)
-        if not t.is_cuda or t.numel() != 1 or t.dtype.itemsize != 4 or t.dtype.is_floating_point:
+        if t.numel() != 1 or t.dtype.itemsize != 4 or t.dtype.is_floating_point:
             raise ValueError("iteration_dev must be a device tensor of one 32-bit integer")
+        _types or _load_types()
+        _here(t, "iteration_dev")
         return _pack_draws(self.seed, self.stream_id, self.iteration, self.row_base, 0, t.data_ptr())
 
 
@@ -525,7 +527,8 @@ def qsgd_pipeline_step(pipe: Pipeline, p: Params, chunk_elems: int, grads, eta: 
 
 # ---- a layer in 8 bits ------------------------------------------------------------
 
-_types = None   # torch dtype -> QSGD_TYPE_*
+_types = None            # torch dtype -> QSGD_TYPE_*
+_current_device = None
 
 
 def _matrix(t, what: str):
@@ -536,8 +539,9 @@ def _matrix(t, what: str):
     if kind is None:
         raise ValueError(f"{what} must be float32, bfloat16, float16 or int8")
     shape = t.shape
-    if len(shape) != 2 or not t.is_cuda:
-        raise ValueError(f"{what} must be a device tensor of two dimensions")
+    if len(shape) != 2:
+        raise ValueError(f"{what} must have two dimensions")
+    _here(t, what)
     rows, cols = shape
     ld, step = t.stride()
     if kind == 3:
@@ -556,9 +560,19 @@ def _matrix(t, what: str):
     return _pack_matrix(t.data_ptr(), rows, cols, ld, kind, 0)
 
 
+def _here(t, what: str) -> None:
+    """Refuses a tensor that is not on the current device, where the kernels run."""
+    d = t.get_device()
+    if d < 0:
+        raise ValueError(f"{what} must be a device tensor")
+    if d != _current_device():
+        raise ValueError(f"{what} is not on the current device")
+
+
 def _load_types():
-    global _types
+    global _types, _current_device
     import torch
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int8: 3}
     return _types
 
@@ -568,8 +582,9 @@ def _vector(t, n: int, what: str):
     if t is None:
         return None
     types = _types or _load_types()
-    if types.get(t.dtype) != 0 or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+    if types.get(t.dtype) != 0 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous device tensor of {n} float32")
+    _here(t, what)
     return t.data_ptr()
 
 

@@ -32,19 +32,36 @@ bool sound(const qsgd_matrix* m, bool levels) {
 
 bool shaped(const qsgd_matrix* m, uint64_t rows, uint64_t cols) { return m->rows == rows && m->cols == cols; }
 
-// Bytes [first, second) that a matrix covers.
+// Bytes [from, to) that something covers.
 struct Span { uintptr_t from, to; };
 Span span(const qsgd_matrix* m) {
   const uintptr_t p = reinterpret_cast<uintptr_t>(m->data_dev);
   if (!m->rows || !m->cols) return {p, p};
   return {p, p + ((m->rows - 1) * m->ld + m->cols) * size_of(m->type)};
 }
+bool meet(const Span& a, const Span& b) { return a.from < b.to && b.from < a.to; }
+// Whether two matrices share an element.  Column ranges of one larger matrix (rows equally far apart) do not where the
+// ranges are apart; other matrices whose extents meet count as overlapping.
 bool overlap(const qsgd_matrix* x, const qsgd_matrix* y) {
   const Span a = span(x), b = span(y);
-  return a.from < b.to && b.from < a.to;
+  if (!meet(a, b)) return false;
+  const uint64_t ld = x->ld * size_of(x->type);
+  if (ld != y->ld * size_of(y->type)) return true;
+  const uint64_t wx = x->cols * size_of(x->type), wy = y->cols * size_of(y->type);
+  const uint64_t d = a.from <= b.from ? (b.from - a.from) % ld : (ld - (a.from - b.from) % ld) % ld;
+  return d < wx || d + wy > ld;
 }
 bool same_place(const qsgd_matrix* x, const qsgd_matrix* y) {
   return x->data_dev == y->data_dev && (x->ld == y->ld || x->rows <= 1);
+}
+// Whether n floats at p share a byte with a matrix.
+bool overlap(const float* p, uint64_t n, const qsgd_matrix* m) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  return p && m && meet({at, at + 4 * n}, span(m));
+}
+bool overlap(const float* p, uint64_t n, const float* q, uint64_t m) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return p && q && meet({a, a + 4 * n}, {b, b + 4 * m});
 }
 
 bool floats(const float* p, uint64_t n) { return n == 0 || (p && aligned(p, 4)); }
@@ -54,6 +71,8 @@ int draw_args(const qsgd_draws* d, uint64_t rows, DrawArgs& a) {
   a = {(uint32_t)d->seed, (uint32_t)(d->seed >> 32), d->stream_id, d->iteration, d->row_base, d->iteration_dev};
   return QSGD_OK;
 }
+
+constexpr uint64_t kMostThreads = 0xFFFF0000ull;   // of a launch: they are counted in 32 bits
 
 int status(hipError_t e) { return e == hipSuccess ? QSGD_OK : QSGD_ERR_HIP; }
 
@@ -67,7 +86,7 @@ int dropout(const qsgd_draws* draws, float p, const qsgd_matrix* x, const qsgd_m
   if (residual && overlap(residual, y) && !same_place(residual, y)) return QSGD_ERR_INVALID_ARG;
   DropoutArgs a = {};
   if (int rc = draw_args(draws, x->rows, a.draws)) return rc;
-  if (x->rows * ((x->cols + 7) / 8) > 0xFFull << 31) return QSGD_ERR_UNSUPPORTED;
+  if (x->rows * ((x->cols + 7) / 8) >= kMostThreads) return QSGD_ERR_UNSUPPORTED;
   if (x->rows == 0 || x->cols == 0) return QSGD_OK;
   a.x = x->data_dev; a.x_ld = x->ld;
   a.y = y->data_dev; a.y_ld = y->ld;
@@ -117,6 +136,7 @@ void want_columns(QuantizeArgs& q, uint8_t* ws, int8_t* levels, uint64_t ld, flo
 
 int quantize(QuantizeJobs& jobs, uint32_t type, uint32_t rounding, hipStream_t st) {
   const bool stochastic = rounding == QSGD_ROUND_STOCHASTIC;
+  if (plan_quantize(jobs, type) * 256 >= kMostThreads) return QSGD_ERR_UNSUPPORTED;
   {
     ScopedTiming tm("quantize_rows", st);
     if (int rc = status(launch_quantize(jobs, type, stochastic, st, false))) return rc;
@@ -131,7 +151,9 @@ int quantize(QuantizeJobs& jobs, uint32_t type, uint32_t rounding, hipStream_t s
 // ---- product ---------------------------------------------------------------------
 
 constexpr uint64_t kMostLd = 1ull << 23;
+constexpr uint64_t kMostRows = 1ull << 26;      // of an operand
 constexpr uint64_t kMostResults = 1ull << 38;   // of one product: workgroups are counted in 31 bits
+bool too_many(uint64_t M, uint64_t N) { return M >= kMostRows || N >= kMostRows || (N && M >= kMostResults / N); }
 
 int product(ProductArgs& p, const ProductPlan& plan, uint8_t* ws, hipStream_t st) {
   p.splits = plan.splits; p.split_k = plan.split_k;
@@ -161,7 +183,6 @@ bool plan_pair(ProductPair& pair, ProductPlan (&plans)[2]) {
   return true;
 }
 
-bool too_many(uint64_t M, uint64_t N) { return N && M >= kMostResults / N; }
 
 // Rows of the workspace's levels start at cache lines (8192 x 8192 x 8000: 440 us per 8192 of k with them, 493 without).
 uint64_t levels_ld(uint64_t k) { return (k + 127) / 128 * 128; }
@@ -169,7 +190,7 @@ uint64_t levels_ld(uint64_t k) { return (k + 127) / 128 * 128; }
 bool in_range(uint64_t a, uint64_t b, uint64_t c) { return a < 1ull << 31 && b < 1ull << 31 && c < 1ull << 31; }
 
 ProductPlan product_plan(uint64_t M, uint64_t N, uint64_t K) {
-  if (!M || !N || M >= kMostResults / N || K >= kMostLd) return {};   // (nothing to do, or refused)
+  if (!M || !N || too_many(M, N) || K >= kMostLd) return {};   // (nothing to do, or refused)
   return plan_product((uint32_t)M, (uint32_t)N, (uint32_t)K);
 }
 uint64_t product_bytes(uint64_t M, uint64_t N, uint64_t K) { return product_plan(M, N, K).bytes; }
@@ -244,12 +265,16 @@ int qsgd_quantize(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix*
   if (columns && (!sound(columns, true) || !shaped(columns, x->cols, x->rows) || !floats(column_scale_dev, x->cols) ||
                   overlap(x, columns) || (rows && overlap(rows, columns))))
     return QSGD_ERR_INVALID_ARG;
+  const float *rs = rows ? row_scale_dev : nullptr, *cs = columns ? column_scale_dev : nullptr;
+  if (overlap(rs, x->rows, cs, x->cols)) return QSGD_ERR_INVALID_ARG;
+  for (const qsgd_matrix* m : {x, rows, columns})
+    if (overlap(rs, x->rows, m) || overlap(cs, x->cols, m)) return QSGD_ERR_INVALID_ARG;
   DrawArgs d = {};
   if (rounding == QSGD_ROUND_STOCHASTIC || draws)
     if (int rc = draw_args(draws, x->rows, d)) return rc;
   const uint64_t need = columns ? qsgd_quantize_workspace_bytes(x->rows, x->cols) : 0;
   if (!room(workspace_dev, workspace_bytes, need)) return no_room(workspace_dev, need);
-  QuantizeJobs jobs = {1, {job(x, d)}};
+  QuantizeJobs jobs = {1, {}, {job(x, d)}};
   if (rows && x->rows) want_rows(jobs.job[0], reinterpret_cast<int8_t*>(rows->data_dev), rows->ld, row_scale_dev);
   if (columns && x->cols)
     want_columns(jobs.job[0], reinterpret_cast<uint8_t*>(workspace_dev), reinterpret_cast<int8_t*>(columns->data_dev),
@@ -265,7 +290,8 @@ int qsgd_int_matmul(const qsgd_matrix* a, const float* a_scale_dev, const qsgd_m
                     const float* bias_dev, const qsgd_matrix* y, void* workspace_dev, size_t workspace_bytes,
                     void* hip_stream) {
   if (!sound(a, true) || !sound(b, true) || !sound(y, false) || a->cols != b->cols || !shaped(y, a->rows, b->rows) ||
-      !floats(a_scale_dev, a->rows) || !floats(b_scale_dev, b->rows) || !aligned(bias_dev, 4) || overlap(a, y) || overlap(b, y))
+      !floats(a_scale_dev, a->rows) || !floats(b_scale_dev, b->rows) || !aligned(bias_dev, 4) || overlap(a, y) || overlap(b, y) ||
+      overlap(a_scale_dev, a->rows, y) || overlap(b_scale_dev, b->rows, y) || overlap(bias_dev, b->rows, y))
     return QSGD_ERR_INVALID_ARG;
   if (a->ld >= kMostLd || b->ld >= kMostLd || too_many(y->rows, y->cols)) return QSGD_ERR_UNSUPPORTED;
   if (y->rows == 0 || y->cols == 0) return QSGD_OK;
@@ -290,7 +316,7 @@ int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_m
                         size_t workspace_bytes, void* hip_stream) {
   if (rounding > QSGD_ROUND_STOCHASTIC || !sound(x, false) || !sound(w, true) || !sound(y, false) || x->cols != w->cols ||
       !shaped(y, x->rows, w->rows) || y->type != x->type || !floats(w_scale_dev, w->rows) || !aligned(bias_dev, 4) ||
-      overlap(x, y) || overlap(w, y))
+      overlap(x, y) || overlap(w, y) || overlap(w_scale_dev, w->rows, y) || overlap(bias_dev, w->rows, y))
     return QSGD_ERR_INVALID_ARG;
   if (w->ld >= kMostLd || levels_ld(x->cols) >= kMostLd || too_many(y->rows, y->cols)) return QSGD_ERR_UNSUPPORTED;
   DrawArgs d = {};
@@ -311,7 +337,7 @@ int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_m
     return status(launch_linear_few({p, x->data_dev, x->ld, d}, x->type, rounding == QSGD_ROUND_STOCHASTIC, st));
   }
   const uint64_t ld = levels_ld(x->cols);
-  QuantizeJobs jobs = {1, {job(x, d)}};
+  QuantizeJobs jobs = {1, {}, {job(x, d)}};
   QuantizeArgs& q = jobs.job[0];
   want_rows(q, reinterpret_cast<int8_t*>(ws), ld, reinterpret_cast<float*>(ws + s.scale));
   if (int rc = quantize(jobs, x->type, rounding, st)) return rc;
@@ -339,6 +365,8 @@ int qsgd_linear_backward(const qsgd_draws* draws, uint32_t rounding, const qsgd_
     for (const auto* i : in)
       if (o && overlap(o, i)) return QSGD_ERR_INVALID_ARG;
   if (dx && dw && overlap(dx, dw)) return QSGD_ERR_INVALID_ARG;
+  for (const qsgd_matrix* m : {x, w, dy, dx, dw})
+    if (overlap(db_dev, w->rows, m)) return QSGD_ERR_INVALID_ARG;
   const uint64_t M = x->rows, N = w->rows, K = x->cols;
   if (levels_ld(N) >= kMostLd || levels_ld(M) >= kMostLd || too_many(M, K) || too_many(N, K)) return QSGD_ERR_UNSUPPORTED;
   DrawArgs d = {};

@@ -157,16 +157,18 @@ struct QuantizeArgs {
   uint32_t* part_max;         // chunks x cols: largest magnitude's bits as fp32; or null: no column form
   float* part_sum;            // chunks x cols, or null: sums of the columns
   float* col_sum;             // where the sums go
-  // workgroups (launch_quantize)
+  // workgroups (plan_quantize)
   uint32_t row_lanes, row_blocks, max_blocks, tile_blocks;
   bool stream;                // the second launch reads x past the caches
   uint32_t tile_rows;         // rows that a workgroup of the second launch takes, a multiple of 128
 };
-struct QuantizeJobs { uint32_t count; QuantizeArgs job[3]; };
+struct QuantizeJobs { uint32_t count, blocks[2]; QuantizeArgs job[3]; };   // blocks: of the two launches
 // Lanes to a row of a strip of columns, rows of a chunk, and how many chunks there are.
 void plan_columns(uint32_t rows, uint32_t cols, uint32_t& strip_lanes, uint32_t& chunks, uint32_t& chunk_rows);
+// Fills in the workgroups of both launches and says how many the larger one has.
+uint64_t plan_quantize(QuantizeJobs& jobs, uint32_t type);
 // First launch: row forms, and the columns' maxima and sums; second: column forms.
-hipError_t launch_quantize(QuantizeJobs& jobs, uint32_t type, bool stochastic, hipStream_t st, bool second);
+hipError_t launch_quantize(const QuantizeJobs& jobs, uint32_t type, bool stochastic, hipStream_t st, bool second);
 
 // ---- product -----------------------------------------------------------------------
 struct ProductArgs {

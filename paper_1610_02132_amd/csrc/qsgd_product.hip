@@ -511,6 +511,7 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
   };
   for (const Kernel& k : kernels) {
     const double tiles = (double)((M + k.size - 1) / k.size) * ((N + k.size - 1) / k.size), slots = kCus * k.slots;
+    if (tiles >= 1 << 23 && k.kind != kProductTile256) continue;   // (a launch has fewer than 2^32 threads)
     for (uint32_t splits = fewest; splits <= 16 * fewest; splits *= 2) {
       if (splits > fewest && (K / splits < 1024 || tiles * splits > 2 * kCus)) break;
       const double stages = std::ceil(K / 128.0 / splits), groups = tiles * splits;

@@ -285,35 +285,36 @@ void plan_columns(uint32_t rows, uint32_t cols, uint32_t& strip_lanes, uint32_t&
   chunks = (rows + chunk_rows - 1) / chunk_rows;
 }
 
-hipError_t launch_quantize(QuantizeJobs& jobs, uint32_t type, bool stochastic, hipStream_t st, bool second) {
-  uint64_t blocks = 0;
+uint64_t plan_quantize(QuantizeJobs& jobs, uint32_t type) {
+  uint64_t first = 0, second = 0;
   for (uint32_t j = 0; j < jobs.count; ++j) {
     QuantizeArgs& a = jobs.job[j];
-    if (second) {
-      const bool any = a.chunks && (a.part_max || a.part_sum);
-      const uint64_t strips = (a.cols + 63) / 64;
-      // the last reading of a matrix that L2 does not hold goes past the caches (gradients of 8192 tokens, 4096 -> 4096
-      // bf16: 360 us without, 347 with)
-      a.stream = (uint64_t)a.rows * a.cols * (type == QSGD_TYPE_F32 ? 4 : 2) >= 32ull << 20;
-      // every workgroup reads the chunks' maxima: few rows to one only where there would be too few of them
-      // (2047 x 1001, both forms, the whole call: 128 rows 16.1 us, 512 rows 22.2; 8192 x 4096 the same)
-      a.tile_rows = 512;
-      while (a.tile_rows > 128 && strips * ((a.rows + a.tile_rows - 1) / a.tile_rows) < 1024) a.tile_rows /= 2;
-      const uint64_t down = a.part_max ? (a.rows + a.tile_rows - 1) / a.tile_rows : 1;
-      const uint64_t n = a.part_max || a.part_sum ? strips * (any ? down : 1) : 0;
-      if (n > 0x7FFFFFFFull) return hipErrorInvalidValue;
-      a.tile_blocks = (uint32_t)n;
-      blocks += n;
-    } else {
-      a.row_lanes = a.cols <= 8 * 64 * kHeld && a.rows >= 1024 ? 64 : 256;   // a wavefront to a row, or four
-      a.row_blocks = !a.q_rows && !a.row_scale ? 0 : a.row_lanes == 64 ? (a.rows + 3) / 4 : a.rows;
-      a.max_blocks = a.part_max || a.part_sum ? (a.cols + 8 * a.strip_lanes - 1) / (8 * a.strip_lanes) * a.chunks : 0;
-      blocks += (uint64_t)a.row_blocks + a.max_blocks;
-    }
+    const bool columns = a.part_max || a.part_sum;
+    a.row_lanes = a.cols <= 8 * 64 * kHeld && a.rows >= 1024 ? 64 : 256;   // a wavefront to a row, or four
+    const uint64_t rows = !a.row_scale ? 0 : a.row_lanes == 64 ? (a.rows + 3) / 4 : a.rows;
+    const uint64_t maxima = columns ? (a.cols + 8 * a.strip_lanes - 1) / (8 * a.strip_lanes) * (uint64_t)a.chunks : 0;
+    const uint64_t strips = (a.cols + 63) / 64;
+    // the last reading of a matrix that L2 does not hold goes past the caches (gradients of 8192 tokens, 4096 -> 4096
+    // bf16: 360 us without, 347 with)
+    a.stream = (uint64_t)a.rows * a.cols * (type == QSGD_TYPE_F32 ? 4 : 2) >= 32ull << 20;
+    // every workgroup reads the chunks' maxima: few rows to one only where there would be too few of them
+    // (2047 x 1001, both forms, the whole call: 128 rows 16.1 us, 512 rows 22.2; 8192 x 4096 the same)
+    a.tile_rows = 512;
+    while (a.tile_rows > 128 && strips * ((a.rows + a.tile_rows - 1) / a.tile_rows) < 1024) a.tile_rows /= 2;
+    // (sums alone, and the scales of no rows, need a workgroup to a strip)
+    const uint64_t tiles = !columns ? 0 : strips * (a.part_max && a.rows ? (a.rows + a.tile_rows - 1) / a.tile_rows : 1);
+    a.row_blocks = (uint32_t)rows; a.max_blocks = (uint32_t)maxima; a.tile_blocks = (uint32_t)tiles;
+    first += rows + maxima;
+    second += tiles;
   }
+  jobs.blocks[0] = (uint32_t)first; jobs.blocks[1] = (uint32_t)second;
+  return first > second ? first : second;
+}
+
+hipError_t launch_quantize(const QuantizeJobs& jobs, uint32_t type, bool stochastic, hipStream_t st, bool second) {
+  const uint32_t blocks = jobs.blocks[second];
   if (blocks == 0) return hipSuccess;
-  if (blocks > 0x7FFFFFFFull) return hipErrorInvalidValue;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(256), 0, st, jobs); };
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, st, jobs); };
   auto pick = [&](auto type_c) {
     constexpr uint32_t T = decltype(type_c)::value;
     if (second) stochastic ? go(k_quantize_columns<T, true>) : go(k_quantize_columns<T, false>);

@@ -71,6 +71,18 @@ def test_dropout_does_not_depend_on_layout(dtype, ld, start):
     assert torch.equal(rs, want)
 
 
+def test_dropout_between_columns_of_one_matrix():
+    """Column ranges of a larger matrix: they do not overlap, however close."""
+    big = R.values(50, 96, torch.bfloat16, 5, ld=96).contiguous()
+    want = torch.empty(50, 32, dtype=torch.bfloat16, device="cuda")
+    q.qsgd_dropout(D, 0.2, big[:, :32], want, residual=big[:, 64:])
+    keep = big.clone()
+    q.qsgd_dropout(D, 0.2, big[:, :32], big[:, 32:64], residual=big[:, 64:])
+    assert torch.equal(big[:, 32:64], want) and torch.equal(big[:, :32], keep[:, :32]) and torch.equal(big[:, 64:], keep[:, 64:])
+    with pytest.raises(q.QsgdError):
+        q.qsgd_dropout(D, 0.2, big[:, :32], big[:, 31:63])
+
+
 def test_dropout_drops_whatever_the_value_is():
     """Infinities and NaN in dropped places leave nothing; in kept ones they stay."""
     x = torch.full((64, 512), float("nan"), device="cuda")
@@ -263,11 +275,50 @@ def test_product(M, N, K):
         R.check(y, want, tol, NAME[dtype])
 
 
-def test_product_of_no_depth_is_the_bias():
-    a, b = int_levels(5, 0, 1), int_levels(7, 0, 2)
-    bias = torch.arange(7.0, device="cuda")
-    assert torch.equal(multiplied(a, scales(5, 1), b, scales(7, 2), torch.float32, bias), bias.expand(5, 7))
-    assert bool((multiplied(a, scales(5, 1), b, scales(7, 2), torch.float32) == 0).all())
+def on_device(a, sa, b, sb):
+    """The product in 64 bits on the device (sums below 2^53: exact), and its tolerance in fp32."""
+    y = torch.matmul(a.double().contiguous(), b.double().t().contiguous()) * sa.double()[:, None] * sb.double()
+    return y, 3 * R.U32 * y.abs() * 1.01 + R.LEAST[torch.float32] + R.U32 * y.abs()
+
+
+# sizes that go to each of the kernels, with depths that end in, before and behind every stage of its loop
+DEPTHS = ([(20, 300, 256 * j + r) for j in range(0, 18, 4) for r in (1, 15, 16, 255)] +
+          [(200, 300, 128 * j + r) for j in range(0, 20) for r in (0, 1, 100, 127) if 128 * j + r > 0] +
+          [(1024, 4096, 128 * j + r) for j in range(4, 10) for r in (0, 127)] + [(1030, 4090, 1000), (2500, 2500, 300), (2500, 2470, 129)] +
+          [(4096, 4096, 128 * j + r) for j in range(11, 15) for r in (0, 1)] + [(4090, 4095, 1500), (5000, 5000, 2001)])
+
+
+@pytest.mark.parametrize("M,N", sorted(set(d[:2] for d in DEPTHS)), ids=str)
+def test_product_depths(M, N):
+    most = max(K for m, n, K in DEPTHS if (m, n) == (M, N))
+    big_a, big_b = int_levels(M, most, 1, full=True), int_levels(N, most, 2, full=True)
+    sa, sb = scales(M, 3), scales(N, 4)
+    for K in [K for m, n, K in DEPTHS if (m, n) == (M, N)]:
+        a, b = big_a[:, :K], big_b[:, :K]
+        y = multiplied(a, sa, b, sb, torch.float32)
+        want, tol = on_device(a, sa, b, sb)
+        assert bool(((y.double() - want).abs() <= tol).all()), K
+
+
+def test_product_in_pieces():
+    """Depths that are summed in pieces and joined, results four to a thread and one."""
+    for M, N, K in ((64, 64, 8192), (33, 70, 20_000), (50, 71, 9001), (1500, 1500, 20_000), (300, 302, 16_384)):
+        assert q.qsgd_int_matmul_workspace_bytes(M, N, K) > 0
+        a, b = int_levels(M, K, 1, full=True), int_levels(N, K, 2, full=True)
+        sa, sb = scales(M, 3), scales(N, 4)
+        bias = torch.linspace(-2, 2, N, device="cuda")
+        y = multiplied(a, sa, b, sb, torch.float32, bias)
+        want, tol = on_device(a, sa, b, sb)
+        want = want + bias.double()
+        assert bool(((y.double() - want).abs() <= tol + R.U32 * want.abs()).all()), (M, N, K)
+
+
+@pytest.mark.parametrize("M,N", [(5, 7), (40, 70), (300, 500)], ids=str)
+def test_product_of_no_depth_is_the_bias(M, N):
+    a, b = int_levels(M, 0, 1), int_levels(N, 0, 2)
+    bias = torch.arange(float(N), device="cuda")
+    assert torch.equal(multiplied(a, scales(M, 1), b, scales(N, 2), torch.float32, bias), bias.expand(M, N))
+    assert bool((multiplied(a, scales(M, 1), b, scales(N, 2), torch.float32) == 0).all())
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 3, 300_000), (5, 9, 131_072), (70, 40, 131_009), (2, 2, 1_000_003)], ids=str)
@@ -284,12 +335,13 @@ def test_product_sums_past_32_bits(M, N, K):
     R.check(y, want, R.U32 * np.abs(want))
 
 
-def test_product_scales_at_the_ends_of_the_range():
+@pytest.mark.parametrize("times", (1, 7, 200), ids=str)
+def test_product_scales_at_the_ends_of_the_range(times):
     """Scales whose product, or whose product with the sum, leaves fp32 while the result does not; NaN and zero rows."""
-    a, b = int_levels(6, 64, 1), int_levels(6, 64, 2)
+    a, b = int_levels(6 * times, 64, 1), int_levels(6 * times, 64, 2)
     a.fill_(100), b.fill_(100)
-    sa = torch.tensor([2.0 ** -120, 2.0 ** 120, 0.0, 1.0, float("nan"), 1e-30], device="cuda")
-    sb = torch.tensor([2.0 ** 120, 2.0 ** -120, 1.0, 1e-30, 1.0, float("nan")], device="cuda")
+    sa = torch.tensor([2.0 ** -120, 2.0 ** 120, 0.0, 1.0, float("nan"), 1e-30] * times, device="cuda")
+    sb = torch.tensor([2.0 ** 120, 2.0 ** -120, 1.0, 1e-30, 1.0, float("nan")] * times, device="cuda")
     y = multiplied(a, sa, b, sb, torch.float32)
     with np.errstate(all="ignore"):
         want = 640000.0 * sa.double().cpu().numpy()[:, None] * sb.double().cpu().numpy()[None]
@@ -335,6 +387,20 @@ def test_linear_forward(M, N, K, dtype):
                               None if b is None else b.cpu().numpy(), scale_roundings=1)
         R.check(y, want, tol)
         assert R.outside_untouched(buf, y) and space_kept(wsbuf, need)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 4096, 4096), (1, 300, 47_000), (3, 77, 1000), (4, 500, 8192), (7, 33, 129), (16, 64, 2700),
+                                   (16, 100, 255), (16, 8192, 2048), (40, 300, 512)], ids=str)
+def test_linear_forward_is_quantizer_and_product(M, N, K):
+    """Bit for bit, whichever way it takes."""
+    for dtype, rounding in zip(TYPES, (1, 0, 1)):
+        x, w, ws = R.values(M, K, dtype, 1), int_levels(N, K, 2), scales(N, 3)
+        bias = torch.linspace(-1, 1, N, device="cuda")
+        work = torch.empty(q.qsgd_linear_forward_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
+        y = torch.empty(M, N, dtype=dtype, device="cuda")
+        q.qsgd_linear_forward(D, x, w, ws, y, bias=bias, workspace=work, rounding=rounding)
+        got = quantized(x, rounding, "rows")
+        assert torch.equal(y, multiplied(got["rows"], got["row_scale"], w, ws, dtype, bias))
 
 
 def test_linear_forward_rows_without_a_scale():

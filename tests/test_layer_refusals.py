@@ -69,6 +69,18 @@ def test_dropout_refusals(b):
     assert L.qsgd_dropout_backward(ref(draws(b)), 2.0, ref(mat(b, A, 4, 32)), ref(mat(b, Y, 4, 32)), None) == INVALID
 
 
+def test_work_that_a_launch_cannot_count(b):
+    L = b._load()
+    x, y = mat(b, A, 2 ** 30, 64, BF16), mat(b, A + 2 ** 40, 2 ** 30, 64, BF16)
+    assert L.qsgd_dropout(draws(b), 0.1, x, None, y, None) == UNSUPPORTED
+    rows = mat(b, A + 2 ** 42, 2 ** 25, 4096, I8)
+    assert L.qsgd_quantize(None, 0, mat(b, A, 2 ** 25, 4096, BF16), rows, 2 ** 45, None, None, None, 0, None) == UNSUPPORTED
+    a, w = mat(b, A, 2 ** 26, 16, I8), mat(b, A + 2 ** 40, 16, 16, I8)
+    assert L.qsgd_int_matmul(a, 2 ** 45, w, 2 ** 44, None, mat(b, A + 2 ** 42, 2 ** 26, 16), None, 0, None) == UNSUPPORTED
+    a, w = mat(b, A, 2 ** 20, 16, I8), mat(b, A + 2 ** 40, 2 ** 18, 16, I8)
+    assert L.qsgd_int_matmul(a, 2 ** 45, w, 2 ** 44, None, mat(b, A + 2 ** 42, 2 ** 20, 2 ** 18), None, 0, None) == UNSUPPORTED
+
+
 def test_nothing_to_do_is_no_error(b):
     """Matrices without elements: nothing is launched (there need not be a GPU)."""
     L = b._load()
@@ -107,6 +119,9 @@ def test_quantize_refusals(b):
     assert call(cols=mat(b, Y, 8, 40, I8, ld=48)) == INVALID          # the column form is transposed
     assert call(rows=mat(b, A, 8, 40, I8, ld=48)) == INVALID          # overlaps x
     assert call(cols=mat(b, B, 40, 8, I8, ld=16)) == INVALID          # overlaps the row form
+    assert call(rs=A + 64) == INVALID                                 # scales over x, over levels, over each other
+    assert call(cs=B + 16) == INVALID
+    assert call(cs=Z + 16) == INVALID
     assert call(ws=None) == INVALID
     assert call(ws=W + 8) == INVALID
     assert call(size=need - 1) == CAPACITY
@@ -132,6 +147,9 @@ def test_product_refusals(b):
     assert call(y=mat(b, Y, 24, 8)) == INVALID
     assert call(y=mat(b, Y, 8, 24, I8, ld=32)) == INVALID
     assert call(y=mat(b, A, 8, 24)) == INVALID                        # overlaps an operand
+    assert call(sa=Y + 64) == INVALID                                 # ... or its scales, or the bias
+    assert call(sb=Y + 64) == INVALID
+    assert call(bias=Y + 64) == INVALID
     assert call(a=mat(b, A, 8, 40, I8, ld=2 ** 23)) == UNSUPPORTED
     K = 200_000
     long = b.qsgd_int_matmul_workspace_bytes(8, 24, K)                # sums that pass 32 bits are joined from pieces
@@ -186,6 +204,7 @@ def test_linear_refusals(b):
     assert backward(dx=mat(b, A, M, K, BF16)) == INVALID              # over x
     assert backward(dw=mat(b, Y + 64, N, K, F32)) == INVALID          # over dx
     assert backward(db=Z + 2) == INVALID
+    assert backward(db=Y + 64) == INVALID                             # over dx
     assert backward(ws=W + 4) == INVALID
     assert backward(size=need_b - 1) == CAPACITY
     assert backward(d=draws(b, row_base=2 ** 32 - 7)) == INVALID
