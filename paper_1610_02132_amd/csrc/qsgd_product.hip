@@ -487,16 +487,17 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
 // Which kernel, and in how many pieces of k: the one that is expected to take the least time (us).  A tile kernel's
 // workgroups run in rounds of as many as the 256 compute units hold; a round takes a fixed time and one per stage of
 // 128 bytes of k, longer where several workgroups share a compute unit.  Few rows: the weights' bytes, a's rows that
-// every workgroup reads anew, and the turns of a wavefront.  Fitted to 62 products from 1 x 1024 x 1024 to 8192^3 that
-// every kernel was timed on: the choice takes at most 6% longer than the fastest on 58 of them, 24% on the worst
-// (us, the choice and the fastest: 2048 x 4096 x 1024 21.7 and 18.6; 1 x 16384 x 1024 6.2 and 5.0).
+// every workgroup reads anew, and the turns of a wavefront.  Fitted to 73 products from 1 x 1024 x 1024 to 8192^3 that
+// every kernel was timed on: the choice takes at most 6% longer than the fastest on 68 of them, 24% on the worst
+// (us, the choice and the fastest: 2048 x 4096 x 1024 20.0 and 19.2 in one run, 21.7 and 18.6 in another; 1 x 16384 x 1024
+// 6.2 and 5.0; 1500 x 1500 x 4096 23.6 and 20.3; 16 x 256 x 8192 9.0 and 7.6).
 ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
   struct Kernel { uint32_t kind, size, slots; double fixed, alone, full; };
   static constexpr Kernel kernels[] = {
       {kProductTile64Deep, 64, 2, 2.3, 0.17, 0.37},
       {kProductTile64, 64, 5, 1.9, 0.24, 1.2},
       {kProductTile128, 128, 2, 3.2, 0.53, 0.97},
-      {kProductTile256, 256, 1, 12.0, 1.3, 1.3},
+      {kProductTile256, 256, 1, 11.4, 1.3, 1.3},
   };
   constexpr double kLaunch = 2.3, kCus = 256.0;
   const uint32_t fewest = std::max(1u, (K + kMostK - 1) / kMostK);
