@@ -487,8 +487,8 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
 // Which kernel, and in how many pieces of k: the one that is expected to take the least time (us).  A tile kernel's
 // workgroups run in rounds of as many as the 256 compute units hold; a round takes a fixed time and one per stage of
 // 128 bytes of k, longer where several workgroups share a compute unit.  Few rows: the weights' bytes, a's rows that
-// every workgroup reads anew, and the turns of a wavefront.  Fitted to 73 products from 1 x 1024 x 1024 to 8192^3 that
-// every kernel was timed on: the choice takes at most 6% longer than the fastest on 68 of them, 24% on the worst
+// every workgroup reads anew, and the turns of a wavefront.  Fitted to 71 products from 1 x 1024 x 1024 to 8192^3 that
+// every kernel was timed on: the choice takes at most 6% longer than the fastest on 67 of them, 24% on the worst
 // (us, the choice and the fastest: 2048 x 4096 x 1024 20.0 and 19.2 in one run, 21.7 and 18.6 in another; 1 x 16384 x 1024
 // 6.2 and 5.0; 1500 x 1500 x 4096 23.6 and 20.3; 16 x 256 x 8192 9.0 and 7.6).
 ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
