@@ -464,22 +464,25 @@ __global__ __launch_bounds__(1024) void k_linear_few(LinearArgs l) {
   }
 }
 
-// The pieces' sums, added in 64 bits: PER neighbouring results of a row to a thread.
+// The pieces' sums, added in 64 bits: PER neighbouring results of a row to a thread, and others behind them where there
+// are more than a launch counts.
+constexpr uint32_t kMostJoinBlocks = 1u << 16;
 template <int PER>
 __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
-  const uint64_t all = (uint64_t)a.M * a.N, i = PER * ((uint64_t)blockIdx.x * 256 + threadIdx.x);
-  if (i >= all) return;
-  int64_t sum[PER] = {};
-  for (uint32_t s = 0; s < a.splits; ++s) {
-    int v[PER];
-    if constexpr (PER == 4) *reinterpret_cast<int4v*>(v) = *reinterpret_cast<const int4v*>(a.part + s * all + i);
-    else v[0] = a.part[s * all + i];
+  const uint64_t all = (uint64_t)a.M * a.N;
+  for (uint64_t i = PER * ((uint64_t)blockIdx.x * 256 + threadIdx.x); i < all; i += PER * 256ull * gridDim.x) {
+    int64_t sum[PER] = {};
+    for (uint32_t s = 0; s < a.splits; ++s) {
+      int v[PER];
+      if constexpr (PER == 4) *reinterpret_cast<int4v*>(v) = *reinterpret_cast<const int4v*>(a.part + s * all + i);
+      else v[0] = a.part[s * all + i];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) sum[e] += v[e];
+      for (int e = 0; e < PER; ++e) sum[e] += v[e];
+    }
+    const uint32_t m = all >> 32 ? (uint32_t)(i / a.N) : (uint32_t)i / a.N, n = (uint32_t)(i - (uint64_t)m * a.N);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) put(a, m, n + e, (float)sum[e], a.a_scale[m]);
   }
-  const uint32_t m = all >> 32 ? (uint32_t)(i / a.N) : (uint32_t)i / a.N, n = (uint32_t)(i - (uint64_t)m * a.N);
-#pragma unroll
-  for (int e = 0; e < PER; ++e) put(a, m, n + e, (float)sum[e], a.a_scale[m]);
 }
 
 }  // namespace
@@ -524,7 +527,7 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
       offer(k.kind, splits, kLaunch + rounds * round(slots) + (left > 0 ? round(left) : 0.0) + join(splits));
     }
   }
-  if (M <= 32)
+  if (M <= 32 && N <= 1u << 25)   // (a launch has fewer than 2^32 threads, here too)
     offer(kProductFew, fewest, kLaunch + 1.4 + (double)N * K / 1.2e7 + (double)M * K * ((N + 15) / 16) / 1.4e7 + 1.3 * std::ceil(K / 4096.0) + join(fewest));
   if (best.splits > 1) best.bytes = (uint64_t)best.splits * M * N * 4;
   return best;
@@ -572,9 +575,10 @@ hipError_t launch_linear_few(const LinearArgs& l, uint32_t type, bool stochastic
 }
 
 hipError_t launch_product_join(const ProductArgs& a, hipStream_t st) {
-  const uint64_t all = (uint64_t)a.M * a.N;
-  if (a.N % 4 == 0) hipLaunchKernelGGL(k_product_join<4>, dim3((uint32_t)((all / 4 + 255) / 256)), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_product_join<1>, dim3((uint32_t)((all + 255) / 256)), dim3(256), 0, st, a);
+  const uint64_t units = (uint64_t)a.M * a.N / (a.N % 4 ? 1 : 4);
+  const dim3 grid((uint32_t)std::min<uint64_t>((units + 255) / 256, kMostJoinBlocks));
+  if (a.N % 4 == 0) hipLaunchKernelGGL(k_product_join<4>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_product_join<1>, grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

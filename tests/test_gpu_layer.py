@@ -313,6 +313,24 @@ def test_product_in_pieces():
         assert bool(((y.double() - want).abs() <= tol + R.U32 * want.abs()).all()), (M, N, K)
 
 
+@pytest.mark.parametrize("M,N", [(8200, 8200), (4100, 4101)], ids=str)
+def test_pieces_of_more_results_than_one_pass_of_a_launch(M, N):
+    """2^26 results four to a thread, 2^24 one to a thread, and some more: the last rows come with a second pass."""
+    K = 130_817
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    ld = (K + 15) // 16 * 16
+    a, b = (torch.randint(-127, 128, (n, ld), generator=g, device="cuda", dtype=torch.int8)[:, :K] for n in (M, N))
+    sa, sb = scales(M, 3), scales(N, 4)
+    y = torch.full((M, N), float("nan"), device="cuda")
+    ws = torch.empty(q.qsgd_int_matmul_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
+    q.qsgd_int_matmul(a, sa, b, sb, y, workspace=ws)
+    assert not bool(y.isnan().any())
+    rows = torch.tensor([0, 1, M // 2, M - 2, M - 1], device="cuda")
+    want, tol = on_device(a[rows], sa[rows], b, sb)
+    assert bool(((y[rows].double() - want).abs() <= tol).all())
+
+
 @pytest.mark.parametrize("M,N", [(5, 7), (40, 70), (300, 500)], ids=str)
 def test_product_of_no_depth_is_the_bias(M, N):
     a, b = int_levels(M, 0, 1), int_levels(N, 0, 2)
