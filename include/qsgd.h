@@ -246,7 +246,8 @@ int qsgd_pipeline_step(qsgd_pipeline *pl, const qsgd_params *p, uint64_t chunk_e
  * nothing and may be captured.  An output or a workspace must not overlap another argument, except where said;
  * outputs that do are refused with QSGD_ERR_INVALID_ARG (column ranges of one larger matrix do not
  * overlap).  QSGD_ERR_UNSUPPORTED: more work than a launch can count (2^32 blocks of eight columns of dropout,
- * 2^24 rows of more than 2048 columns of the quantizer, 2^26 rows of an operand, 2^38 results of a product).
+ * 2^24 rows of more than 2048 columns of the quantizer and 2^26 of any, 2^30 columns quantized by columns, 2^26 rows of
+ * an operand, rows of levels 2^23 bytes apart, 2^38 results of a product).
  */
 
 /* Element types of a matrix. */
@@ -319,7 +320,8 @@ int qsgd_quantize(const qsgd_draws *draws, uint32_t rounding, const qsgd_matrix 
 
 /* Product of 8-bit matrices:  y[m][n] = (sum_k a[m][k] b[n][k]) a_scale[m] b_scale[n] + bias[n].
  * The sum is exact (32-bit integers, joined in 64 bits where they could pass); the factors are
- * applied in fp32, the smaller scale first, and the result is rounded once to y's type.
+ * applied in fp32, a's scale first, b's and the bias in one rounding, and the result is rounded once
+ * to y's type; it overflows only where its value does (a scale below 2^-126 may vanish).
  *   a  M x K, I8, with M scales;  b  N x K, I8, with N scales;  bias_dev  N floats or NULL
  *   y  M x N, F32, BF16 or F16; must not overlap the operands
  *   workspace  device, 16-byte aligned, >= qsgd_int_matmul_workspace_bytes(M, N, K), calls sharing

@@ -19,9 +19,9 @@ constexpr uint32_t kMostK = 130816;
 constexpr uint32_t kSums = 99;   // "type" of a piece's sums in the workspace
 
 // The sum times the row's scale, times the column's, plus the bias, the last two in one rounding.  A row's scale above
-// kBigScale is taken 2^64 times smaller and the product larger again, so that a result overflows only where it has to;
-// the sum is a whole number and the scales are not subnormal, so that nothing vanishes on the way.
-constexpr float kBigScale = 0x1p96f;
+// kBigScale is taken 2^64 times smaller and the product larger again, so that a result overflows only where it has to (a
+// sum is below 2^37); it is a whole number and the scales are not subnormal, so that nothing vanishes on the way.
+constexpr float kBigScale = 0x1p90f;
 __device__ __forceinline__ float result(float sum, float s, float t, float bias) {
   return s > kBigScale ? sum * (s * 0x1p-64f) * t * 0x1p64f + bias : __builtin_fmaf(sum * s, t, bias);
 }

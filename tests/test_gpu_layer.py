@@ -369,6 +369,19 @@ def test_product_scales_at_the_ends_of_the_range(times):
     R.check(np.where(over, 0, g), np.where(over, 0, want), R.U32 * 3 * np.where(over, 0, np.abs(np.nan_to_num(want))) * 1.01 + 2.0 ** -149)
 
 
+@pytest.mark.parametrize("M,N", [(2, 3), (70, 40)], ids=str)
+def test_product_of_long_sums_and_large_scales(M, N):
+    """A sum near 2^37 times a scale of 2^95 leaves fp32, the result of the two scales does not."""
+    K = 8_000_000
+    a, b = (torch.full((n, K), 127, dtype=torch.int8, device="cuda") for n in (M, N))
+    for s, t in ((2.0 ** 95, 2.0 ** -100), (2.0 ** -100, 2.0 ** 95), (2.0 ** 91, 2.0 ** -30), (2.0 ** 89, 1.0)):
+        y = torch.empty(M, N, device="cuda")
+        ws = torch.empty(q.qsgd_int_matmul_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
+        q.qsgd_int_matmul(a, torch.full((M,), s, device="cuda"), b, torch.full((N,), t, device="cuda"), y, workspace=ws)
+        want = K * 127.0 ** 2 * s * t
+        assert bool(((y.double() - want).abs() <= 4 * R.U32 * want).all()), (s, t)
+
+
 def test_product_operands_in_larger_matrices():
     """Column ranges of wider matrices: what stands behind K in a row, levels and all, changes nothing."""
     big_a, big_b = int_levels(90, 400, 1, full=True), int_levels(110, 400, 2, full=True)
