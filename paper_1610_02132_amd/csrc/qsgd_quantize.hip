@@ -167,7 +167,7 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantizeJobs jobs) {
 // levels of one column make a word in LDS; 16 bytes of a column's 128 leave with a lane.
 template <uint32_t TYPE, bool STOCHASTIC>
 __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
-  __shared__ __attribute__((aligned(16))) uint32_t tile[64 * 32];
+  __shared__ __attribute__((aligned(16))) uint32_t tiles[2][64 * 32];   // in turn, with one wait between them
   __shared__ uint32_t found[4][64];
   __shared__ float added[4][64], factor[64];
   uint32_t block = blockIdx.x, j = 0;
@@ -236,7 +236,8 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
   for (int i = 0; i < 8; ++i) inv[i] = factor[8 * cx + i];
   // word w of column n: the 16-byte places of a column change with its number, so that eight threads' words do not meet
   auto at = [&](uint32_t n, uint32_t w) { return 32 * n + 4 * ((w >> 2) ^ (n >> 3 & 7)) + (w & 3); };
-  for (uint32_t r0 = first; r0 < end; r0 += 128) {
+  for (uint32_t r0 = first, turn = 0; r0 < end; r0 += 128, turn ^= 1) {
+    uint32_t* const tile = tiles[turn];
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
       float t[4];
@@ -266,7 +267,6 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
         }
       }
     }
-    __syncthreads();
   }
 }
 
