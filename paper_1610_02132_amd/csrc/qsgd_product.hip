@@ -327,27 +327,37 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPai
 }
 
 // ---- few rows ---------------------------------------------------------------------
-// At most 32 rows of a: the weights' bytes are what it takes.  A workgroup has 16 NT of their rows and up to 16 wavefronts,
-// which take turns at 256 bytes of k; a lane loads 64 of them in a row (the order of k is the same for both
-// operands, so it need not be the matrix instruction's own), straight from memory: no two wavefronts share them.
-constexpr uint32_t kFewDepth = 256;
+// At most 32 rows of a: the weights' bytes are what it takes.  A workgroup has 16 of their rows and up to eight wavefronts,
+// which take turns at 256 bytes of k, loaded whole into a wavefront's own piece of LDS and read from there as the matrix
+// instruction wants them (a lane has 64 bytes in a row: the order of k is the same for both operands, so it need not be
+// the instruction's own).  1 x 28672 x 8192 40.2 us = 5.9 TB/s, the rate of a copy; loads straight into registers, whose lanes are
+// in 16 rows, 42.0; 16 wavefronts 40.9.
+constexpr uint32_t kFewDepth = 256, kFewWaves = 8;
 
-template <int MT, int NT>
-__global__ __launch_bounds__(1024) void k_product_few(ProductArgs a) {
-  __shared__ __attribute__((aligned(16))) int sums[16][MT * NT * 256];
+template <int MT>
+__global__ __launch_bounds__(64 * kFewWaves) void k_product_few(ProductArgs a) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t staged[];   // 4 KiB for each wavefront
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const uint32_t n0 = blockIdx.x * 16 * NT, k0 = blockIdx.y * a.split_k, k1 = min(k0 + a.split_k, a.K);
-  const uint32_t own = 64 * (lane >> 4);
-  int4v acc[MT][NT] = {};
+  const uint32_t n0 = blockIdx.x * 16, k0 = blockIdx.y * a.split_k, k1 = min(k0 + a.split_k, a.K);
+  const uint32_t own = 64 * (lane >> 4), rows = min(16u, a.N - n0), padded = (a.K + 15) / 16 * 16;
+  uint8_t* const place = staged + 4096 * wave;
+  const auto from = __builtin_amdgcn_make_buffer_rsrc((void*)(a.b + n0 * a.b_ld), 0, (int)((rows - 1) * (uint32_t)a.b_ld + padded), 0x27000);
+  // load j of a turn: rows 4 j to 4 j + 3, 256 bytes of each in a row; place s of a row holds chunk s ^ row
+  uint32_t row_at[4], chunk[4];
+#pragma unroll
+  for (uint32_t j = 0; j < 4; ++j) {
+    const uint32_t r = 4 * j + (lane >> 4);
+    row_at[j] = min(r, rows - 1) * (uint32_t)a.b_ld;
+    chunk[j] = 16 * ((lane & 15) ^ r);
+  }
+  int4v acc[MT] = {};
   for (uint32_t k = k0 + wave * kFewDepth; k < k1; k += waves * kFewDepth) {
-    int4v w[NT][4], x[MT][4];
-    if (k + kFewDepth <= k1) {
+    int4v x[MT][4];
+    const bool whole = k + kFewDepth <= k1;
+    const uint32_t end = padded - 16 - k;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const int8_t* p = a.b + (min(n0 + 16 * t + (lane & 15), a.N - 1) * a.b_ld + k + own);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[t][j] = reinterpret_cast<const int4v*>(p)[j];
-      }
+    for (uint32_t j = 0; j < 4; ++j) load_to_lds(from, place + 1024 * j, row_at[j] + (whole ? chunk[j] : min(chunk[j], end)), k);
+    if (whole) {
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
         const int8_t* p = a.a + (min(16 * t + (lane & 15), a.M - 1) * a.a_ld + k + own);
@@ -356,33 +366,32 @@ __global__ __launch_bounds__(1024) void k_product_few(ProductArgs a) {
       }
     } else {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[t][j] = operand(a.b, a.b_ld, n0 + 16 * t + (lane & 15), a.N, k + own + 16 * j, a.K);
-#pragma unroll
       for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           x[t][j] = masked(operand(a.a, a.a_ld, 16 * t + (lane & 15), a.M, k + own + 16 * j, a.K), k + own + 16 * j, a.K);
     }
+    wait_loads<0>();
+    int4v w[4];
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j)
+      w[j] = *reinterpret_cast<const int4v*>(place + 256 * (lane & 15) + 16 * ((4 * (lane >> 4) + j) ^ (lane & 15)));
+    wait_loads<63>();   // (read before the next turn's come)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int u = 0; u < NT; ++u) acc[t][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][j], x[t][j], acc[t][u], 0, 0, 0);
+      for (int t = 0; t < MT; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], x[t][j], acc[t], 0, 0, 0);
   }
+  int* const sums = reinterpret_cast<int*>(staged);
 #pragma unroll
   for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int u = 0; u < NT; ++u)
-      *reinterpret_cast<int4v*>(&sums[wave][(16 * t + (lane & 15)) * (16 * NT) + 16 * u + 4 * (lane >> 4)]) = acc[t][u];
+    *reinterpret_cast<int4v*>(&sums[1024 * wave + (16 * t + (lane & 15)) * 16 + 4 * (lane >> 4)]) = acc[t];
   __syncthreads();
-  for (uint32_t o = threadIdx.x; o < MT * NT * 256; o += blockDim.x) {
-    const uint32_t m = o / (16 * NT), n = n0 + o % (16 * NT);
+  for (uint32_t o = threadIdx.x; o < MT * 256; o += blockDim.x) {
+    const uint32_t m = o / 16, n = n0 + o % 16;
     if (m >= a.M || n >= a.N) continue;
     int sum = 0;
-    for (uint32_t s = 0; s < waves; ++s) sum += sums[s][o];
+    for (uint32_t s = 0; s < waves; ++s) sum += sums[1024 * s + o];
     if (a.part) a.part[((uint64_t)blockIdx.y * a.M + m) * a.N + n] = sum;
     else put(a, m, n, (float)sum, a.a_scale[m]);
   }
@@ -544,9 +553,10 @@ hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t s
   };
   if (kind == kProductFew) {
     const uint32_t steps = (std::min(a.K, a.split_k) + kFewDepth - 1) / kFewDepth;
-    const dim3 block(64 * std::max(1u, std::min(steps, 16u))), grid((a.N + 15) / 16, a.splits);
-    if (a.M <= 16) hipLaunchKernelGGL((k_product_few<1, 1>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((k_product_few<2, 1>), grid, block, 0, st, a);
+    const uint32_t waves = std::max(1u, std::min(steps, kFewWaves)), lds = 4096 * waves;
+    const dim3 block(64 * waves), grid((a.N + 15) / 16, a.splits);
+    if (a.M <= 16) hipLaunchKernelGGL(k_product_few<1>, grid, block, lds, st, a);
+    else hipLaunchKernelGGL(k_product_few<2>, grid, block, lds, st, a);
   }
   else if (kind == kProductTile64Deep) tiles(k_product<1, 1, 4>, 64);
   else if (kind == kProductTile64) tiles(k_product<1, 1, 2>, 64);
@@ -556,11 +566,13 @@ hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t s
 }
 
 // Whether quantizing in every workgroup is the faster way: not where many of them make many levels each, or where the
-// weights have so many rows that the tile kernels read them faster (us, together and apart, bf16, M x N x K: 1 x 4096 x 4096
-// 7.6 / 10.5, 8 x 4096 x 4096 9.6 / 10.6, 1 x 8192 x 8192 15.3 / 18.1, 1 x 16384 x 4096 18.2 / 16.8, 16 x 8192 x 2048 12.1 / 10.6).
+// weights have so many rows that the kernels without it read them faster (us, together and apart, bf16, M x N x K: 1 x 4096 x 4096
+// 8.4 / 11.3, 8 x 4096 x 4096 9.6 / 11.4, 1 x 12288 x 8192 22.9 / 24.1, 1 x 16384 x 4096 18.3 / 16.7, 1 x 28672 x 8192 49.4 / 45.5,
+// 4 x 16384 x 2048 10.5 / 12.2, 2 x 32768 x 2048 15.6 / 16.3, 1 x 65536 x 512 12.9 / 11.4, 16 x 8192 x 2048 12.0 / 11.1).
 // LDS holds 16 KiB of sums and 47 KiB of levels.
 bool linear_few_fits(uint32_t M, uint32_t N, uint32_t K) {
-  return M <= 16 && N <= 8192 && K > 0 && (uint64_t)M * (K + 272) <= 47u << 10 && (uint64_t)M * K * ((N + 15) / 16) <= 12u << 20;
+  return M <= 16 && (N <= 12288 || (N <= 32768 && K <= 2048)) && K > 0 && (uint64_t)M * (K + 272) <= 47u << 10 &&
+         (uint64_t)M * K * ((N + 15) / 16) <= 12u << 20;
 }
 
 hipError_t launch_linear_few(const LinearArgs& l, uint32_t type, bool stochastic, hipStream_t st) {

@@ -421,7 +421,8 @@ def test_linear_forward(M, N, K, dtype):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 4096, 4096), (1, 300, 47_000), (3, 77, 1000), (4, 500, 8192), (7, 33, 129), (16, 64, 2700),
-                                   (16, 100, 255), (16, 8192, 2048), (40, 300, 512)], ids=str)
+                                   (16, 100, 255), (16, 8192, 2048), (40, 300, 512), (3, 12_288, 100), (1, 12_289, 4096),
+                                   (2, 32_768, 2048), (1, 32_769, 48)], ids=str)
 def test_linear_forward_is_quantizer_and_product(M, N, K):
     """Bit for bit, whichever way it takes."""
     for dtype, rounding in zip(TYPES, (1, 0, 1)):
