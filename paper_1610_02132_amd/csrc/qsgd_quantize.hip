@@ -146,20 +146,22 @@ __device__ __forceinline__ void columns_block(const QuantizeArgs& a, uint32_t bl
   }
 }
 
+// The longer workgroups, a column strip's, come first: those of single rows fill in behind them (both forms of 8192 x 4096
+// bf16, stochastic, the whole call: 51.6 us, rows first 55.0; fp32 74.9 and 82.1).
 template <uint32_t TYPE, bool STOCHASTIC>
 __global__ __launch_bounds__(256) void k_quantize_rows(QuantizeJobs jobs) {
   __shared__ uint32_t shared[2 * 256 * 8];
   uint32_t block = blockIdx.x;
   for (uint32_t j = 0; j < jobs.count; ++j) {
     const QuantizeArgs& a = jobs.job[j];
+    if (block < a.max_blocks) return columns_block<TYPE>(a, block, shared);
+    block -= a.max_blocks;
     if (block < a.row_blocks) {
       if (a.row_lanes == 64) rows_block<TYPE, STOCHASTIC, 64>(a, 4 * block, shared);
       else rows_block<TYPE, STOCHASTIC, 256>(a, block, shared);
       return;
     }
     block -= a.row_blocks;
-    if (block < a.max_blocks) return columns_block<TYPE>(a, block, shared);
-    block -= a.max_blocks;
   }
 }
 
