@@ -342,13 +342,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_product_few(ProductArgs a) {
   const uint32_t own = 64 * (lane >> 4), rows = min(16u, a.N - n0), padded = (a.K + 15) / 16 * 16;
   uint8_t* const place = staged + 4096 * wave;
   const auto from = __builtin_amdgcn_make_buffer_rsrc((void*)(a.b + n0 * a.b_ld), 0, (int)((rows - 1) * (uint32_t)a.b_ld + padded), 0x27000);
-  // load j of a turn: rows 4 j to 4 j + 3, 256 bytes of each in a row; place s of a row holds chunk s ^ row
+  // load j of a turn: rows 4 j to 4 j + 3, 256 bytes of each in a row; place s of a row holds chunk s ^ ((row - 4) % 16), so that
+  // neither 16 neighbours nor fours of them from two halves of 32 lanes read one bank
   uint32_t row_at[4], chunk[4];
 #pragma unroll
   for (uint32_t j = 0; j < 4; ++j) {
     const uint32_t r = 4 * j + (lane >> 4);
     row_at[j] = min(r, rows - 1) * (uint32_t)a.b_ld;
-    chunk[j] = 16 * ((lane & 15) ^ r);
+    chunk[j] = 16 * ((lane & 15) ^ ((r - 4) & 15));
   }
   int4v acc[MT] = {};
   for (uint32_t k = k0 + wave * kFewDepth; k < k1; k += waves * kFewDepth) {
@@ -375,7 +376,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_product_few(ProductArgs a) {
     int4v w[4];
 #pragma unroll
     for (uint32_t j = 0; j < 4; ++j)
-      w[j] = *reinterpret_cast<const int4v*>(place + 256 * (lane & 15) + 16 * ((4 * (lane >> 4) + j) ^ (lane & 15)));
+      w[j] = *reinterpret_cast<const int4v*>(place + 256 * (lane & 15) + 16 * ((4 * (lane >> 4) + j) ^ ((lane - 4) & 15)));
     wait_loads<63>();   // (read before the next turn's come)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
