@@ -30,24 +30,28 @@ __device__ __forceinline__ uint32_t nearest_levels(const float (&t)[4]) {
   return pack_bytes<0>(q[0], q[1], q[2], q[3]);
 }
 
-// Up iff (h + 1/2) / 65536 is below the fraction of |t|:  with R = ceil(65536 |t| - 1/2), a whole number that fp32
-// holds exactly (|t| <= 127 + 2^-17, the next number after 127, so that R <= 127 * 65536 and no level passes 127),
-// the level is the upper half of R + 65535 - h.  `left` has 65535 - h.
-__device__ __forceinline__ uint32_t stochastic_levels(const float (&t)[4], const uint32_t (&left)[4]) {
+// floor(x) as a whole number in one instruction, 0 for a NaN.
+__device__ __forceinline__ int floor_int(float x) {
+  int q;
+  asm("v_cvt_flr_i32_f32 %0, %1" : "=v"(q) : "v"(x));
+  return q;
+}
+
+// Up iff (h + 1/2) / 65536 is below the fraction of |t|:  with F = floor(1/2 - 65536 |t|), a whole number that fp32
+// holds exactly (|t| <= 127 + 2^-17, the next number after 127, so that F >= -127 * 65536 and no level passes 127),
+// the level is -((F + h) >> 16).  Takes -t, whose signs say where the byte of F + h is to be negated.
+__device__ __forceinline__ uint32_t stochastic_levels(const float (&minus_t)[4], const uint32_t (&h)[4]) {
   uint32_t q[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    q[i] = (uint32_t)__builtin_ceilf(__builtin_fmaf(fabsf(t[i]), 65536.0f, -0.5f)) + left[i];
-  const uint32_t level = pack_bytes<2>(q[0], q[1], q[2], q[3]);
-  // a byte of ones where t is negative, and the negative of those bytes: no carry leaves bit 7, which is put in last
-  const uint32_t minus = __builtin_amdgcn_perm(__float_as_uint(t[1]), __float_as_uint(t[0]), 0x0C0C0B09u) |
-                         __builtin_amdgcn_perm(__float_as_uint(t[3]), __float_as_uint(t[2]), 0x0B090C0Cu);
-  const uint32_t flipped = level ^ minus;
-  return ((flipped & 0x7F7F7F7Fu) + (minus & 0x01010101u)) ^ (flipped & 0x80808080u);
+    q[i] = (uint32_t)floor_int(__builtin_fmaf(-fabsf(minus_t[i]), 65536.0f, 0.5f)) + h[i];
+  const uint32_t byte = pack_bytes<2>(q[0], q[1], q[2], q[3]);
+  // a byte of ones where t is positive, and the negative of those bytes: no carry leaves bit 7, which is put in last
+  const uint32_t plus = __builtin_amdgcn_perm(__float_as_uint(minus_t[1]), __float_as_uint(minus_t[0]), 0x0C0C0B09u) |
+                        __builtin_amdgcn_perm(__float_as_uint(minus_t[3]), __float_as_uint(minus_t[2]), 0x0B090C0Cu);
+  const uint32_t flipped = byte ^ plus;
+  return ((flipped & 0x7F7F7F7Fu) + (plus & 0x01010101u)) ^ (flipped & 0x80808080u);
 }
-
-// 65535 - h for the draws of column i of a block.
-__device__ __forceinline__ uint32_t draw_left(const HalfWords& h, int i) { return 0xFFFFu - half_word(h, i); }
 
 // The levels of eight neighbours in a row.
 template <uint32_t TYPE, bool STOCHASTIC>
@@ -55,13 +59,13 @@ __device__ __forceinline__ void eight_levels(const Eight<TYPE>& x, float inv, co
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     float t[4];
-    uint32_t left[4];
+    uint32_t draw[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      t[i] = x.value(4 * half + i) * inv;
-      left[i] = STOCHASTIC ? draw_left(h, 4 * half + i) : 0;
+      t[i] = x.value(4 * half + i) * (STOCHASTIC ? -inv : inv);
+      draw[i] = STOCHASTIC ? half_word(h, 4 * half + i) : 0;
     }
-    q[half] = STOCHASTIC ? stochastic_levels(t, left) : nearest_levels(t);
+    q[half] = STOCHASTIC ? stochastic_levels(t, draw) : nearest_levels(t);
   }
 }
 

@@ -54,6 +54,11 @@ __device__ __forceinline__ int4v operand(const int8_t* p, uint64_t ld, uint32_t 
 // registers (MFMA 32x32x32: the weights' rows are the rows, so that a lane holds four neighbouring results of
 // one row of y).  128 bytes of k, whole cache lines, are a stage; STAGES of them are in LDS, loaded straight from memory.
 // Slot s of a row of 128 bytes holds chunk s ^ swizzle(row).
+// 8192^3, tiles of 256: 440 us = 2500 Tops, the matrix units busy in 73% of the cycles at a clock that the power of these
+// products brings down to 1.5 to 1.7 GHz (matrix instructions alone on such values: 3040 Tops).  A tile of 256 reads half as many bytes of LDS for a matrix
+// instruction as one of 128 (4096^3 62 us, 128-tiles 69), which a batch of a few thousand results does not fill the
+// card with; the tiles of 64 are for those, with four stages where a compute unit has no second workgroup to hide
+// the loads of one (256 x 4096 x 4096 10.7 us).
 constexpr uint32_t kDepth = 128;   // bytes of k in a stage
 
 // Rows whose 16-byte chunks of one number are read together (8 or 16 neighbours, or fours of them whose numbers differ
@@ -399,7 +404,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_product_few(ProductArgs a) {
 }
 
 // The layer for few tokens, their quantizing included: every workgroup makes the levels of all of them (in LDS, where
-// its wavefronts' turns find them) while the weights of its first turn are on their way, which costs less than a launch.
+// its wavefronts' turns find them) while the weights of its first turn are on their way, which costs less than a launch
+// (1 x 8192 x 8192 15.2 us, 4.4 TB/s; two launches 17.2).  Bound by the chain from the tokens' maxima to the last product.
 template <uint32_t TYPE, bool STOCHASTIC>
 __global__ __launch_bounds__(1024) void k_linear_few(LinearArgs l) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -475,7 +481,7 @@ __global__ __launch_bounds__(1024) void k_linear_few(LinearArgs l) {
 }
 
 // The pieces' sums, added in 64 bits: PER neighbouring results of a row to a thread, and others behind them where there
-// are more than a launch counts.
+// are more than a launch counts.  Memory bound; mostly a launch (1500 x 1500 in two pieces 5 us with it).
 constexpr uint32_t kMostJoinBlocks = 1u << 16;
 template <int PER>
 __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {

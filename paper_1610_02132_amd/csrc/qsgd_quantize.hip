@@ -2,7 +2,9 @@
 // column of a matrix, levels as signed bytes.  Two launches for any number of matrices: the first makes the row forms and the
 // columns' largest magnitudes (and sums) over chunks of rows, the second the column forms, transposed through LDS.
 // Memory bound: the row form reads a row once, the column form reads the matrix twice (a column does not fit
-// a compute unit).
+// a compute unit).  8192 x 4096 bf16 to the nearest level by rows: 18.7 us = 5.4 TB/s.  With draws the ten rounds of the generator
+// for eight elements cost as much as their levels, and both launches stay behind the memory: gradients of 8192 tokens, 4096 -> 4096
+// bf16, 58 us for 256 MiB (0.54 vector instructions per SIMD and four clocks) and 52 us for 240 MiB (0.92).
 #include "qsgd_layer.hpp"
 #include "qsgd_levels.hpp"
 
@@ -243,13 +245,13 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
       float t[4];
-      uint32_t left[4];
+      uint32_t draw[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        t[i] = x[i].value(n) * inv[n];
-        left[i] = STOCHASTIC ? draw_left(h[i], n) : 0;
+        t[i] = x[i].value(n) * (STOCHASTIC ? -inv[n] : inv[n]);
+        draw[i] = STOCHASTIC ? half_word(h[i], n) : 0;
       }
-      tile[at(8 * cx + n, ry)] = STOCHASTIC ? stochastic_levels(t, left) : nearest_levels(t);
+      tile[at(8 * cx + n, ry)] = STOCHASTIC ? stochastic_levels(t, draw) : nearest_levels(t);
     }
     if (r0 + 128 < end) load(r0 + 128 + 4 * ry);
     __syncthreads();
