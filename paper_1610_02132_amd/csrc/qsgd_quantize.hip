@@ -4,7 +4,7 @@
 // Memory bound: the row form reads a row once, the column form reads the matrix twice (a column does not fit
 // a compute unit).  8192 x 4096 bf16 to the nearest level by rows: 18.7 us = 5.4 TB/s.  With draws the ten rounds of the generator
 // for eight elements cost as much as their levels, and both launches stay behind the memory: gradients of 8192 tokens, 4096 -> 4096
-// bf16, 58 us for 256 MiB (0.54 vector instructions per SIMD and four clocks) and 52 us for 240 MiB (0.92).
+// bf16, 56 us for 256 MiB (a vector instruction in half of a SIMD's four clocks) and 46 us for 240 MiB (in all of them).
 #include "qsgd_layer.hpp"
 #include "qsgd_levels.hpp"
 
@@ -183,20 +183,41 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
   const uint32_t end = min(first + a.tile_rows, a.rows);
   Eight<TYPE> x[4];
   HalfWords h[4];
-  auto load = [&](uint32_t r) {   // four rows' eight columns, and their draws
+  const uint32_t left = c < a.cols ? a.cols - c : 0;
+  auto load = [&](uint32_t r0) {   // eight columns of four of 128 rows, and their draws; the last row again for those behind it
+    using bits = typename Element<TYPE>::bits;
+    const uint32_t r = r0 + 4 * ry;
+    const bits* p[4] = {reinterpret_cast<const bits*>(a.x) + (min(r, end - 1) * a.ld + c)};
+    if (r0 + 128 <= end) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (c < a.cols && r + i < end) {
-        const void* p = element_at<TYPE>(a.x, a.ld, r + i, c);
-        if (a.stream) x[i].template load<true>(p, a.cols - c);
-        else x[i].load(p, a.cols - c);
+      for (int i = 1; i < 4; ++i) p[i] = p[0] + i * a.ld;
+    } else {
+#pragma unroll
+      for (int i = 1; i < 4; ++i) p[i] = p[i - 1] + (r + i < end ? a.ld : 0);
+    }
+    if (left >= 8) {
+      if (a.stream) {
+        asm volatile("");   // (the two ways are not to be made one)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i].template load<true>(p[i], 8);
+        asm volatile("");
       } else {
-        x[i] = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i].load(p[i], 8);
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = {};
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if ((uint32_t)e < left) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i].set(e, p[i][e]);
+        }
     }
     if constexpr (STOCHASTIC) draw_blocks<4>(a.draws, iteration, {r, r + 1, r + 2, r + 3}, {c / 8, c / 8, c / 8, c / 8}, h);
   };
-  if (a.part_max) load(first + 4 * ry);
+  if (a.part_max && first < end) load(first);
   {   // the chunks' maxima and sums, by four threads to a column
     const uint32_t column = c0 + (threadIdx.x & 63), part = threadIdx.x >> 6;
     uint32_t m = 0;
@@ -253,7 +274,7 @@ __global__ __launch_bounds__(256) void k_quantize_columns(QuantizeJobs jobs) {
       }
       tile[at(8 * cx + n, ry)] = STOCHASTIC ? stochastic_levels(t, draw) : nearest_levels(t);
     }
-    if (r0 + 128 < end) load(r0 + 128 + 4 * ry);
+    if (r0 + 128 < end) load(r0 + 128);
     __syncthreads();
 #pragma unroll
     for (uint32_t p = 0; p < 2; ++p) {
