@@ -507,9 +507,9 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
 // workgroups run in rounds of as many as the 256 compute units hold; a round takes a fixed time and one per stage of
 // 128 bytes of k, longer where several workgroups share a compute unit.  Few rows: the weights' bytes, a's rows that
 // every workgroup reads anew, and the turns of a wavefront.  Fitted to 71 products from 1 x 1024 x 1024 to 8192^3 that
-// every kernel was timed on: the choice takes at most 6% longer than the fastest on 67 of them, 24% on the worst
-// (us, the choice and the fastest: 2048 x 4096 x 1024 20.0 and 19.2 in one run, 21.7 and 18.6 in another; 1 x 16384 x 1024
-// 6.2 and 5.0; 1500 x 1500 x 4096 23.6 and 20.3; 16 x 256 x 8192 9.0 and 7.6).
+// every kernel was timed on: the choice takes at most 6% longer than the fastest on 67 of them, 20% on the worst
+// (us, the choice and the fastest: 8 x 500 x 300 5.4 and 4.5, 1500 x 1500 x 4096 23.7 and 20.1, 1024 x 1024 x 32768 52.1 and
+// 47.3, 64 x 1024 x 8192 12.1 and 11.3).
 ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
   struct Kernel { uint32_t kind, size, slots; double fixed, alone, full; };
   static constexpr Kernel kernels[] = {
@@ -544,7 +544,7 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
     }
   }
   if (M <= 32 && N <= 1u << 25)   // (a launch has fewer than 2^32 threads, here too)
-    offer(kProductFew, fewest, kLaunch + 1.4 + (double)N * K / 1.2e7 + (double)M * K * ((N + 15) / 16) / 1.4e7 + 1.3 * std::ceil(K / 4096.0) + join(fewest));
+    offer(kProductFew, fewest, kLaunch + 1.4 + (double)N * K / 1.2e7 + (double)M * K * ((N + 15) / 16) / 1.4e7 + 0.65 * std::ceil(K / 2048.0) + join(fewest));
   if (best.splits > 1) best.bytes = (uint64_t)best.splits * M * N * 4;
   return best;
 }
