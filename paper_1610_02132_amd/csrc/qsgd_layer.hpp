@@ -183,7 +183,7 @@ struct ProductArgs {
   int32_t* part;              // splits x M x N sums, or null with one piece
 };
 enum ProductKind : uint32_t {
-  kProductFew,        // at most 64 rows of a, straight from memory
+  kProductFew,        // at most 32 rows of a
   kProductTile64Deep, // tiles of 64 x 64 results, four stages of k, ...
   kProductTile64,     // ... and two
   kProductTile128,
