@@ -529,10 +529,27 @@ def qsgd_pipeline_step(pipe: Pipeline, p: Params, chunk_elems: int, grads, eta: 
 
 _types = None            # torch dtype -> QSGD_TYPE_*
 _current_device = None
+_raw_stream_of = None    # device -> torch's current stream on it, as a raw handle
 
 
-def _matrix(t, what: str):
-    """A two-dimensional device tensor with contiguous rows as the bytes of a qsgd_matrix (None for None)."""
+def _begin(stream):
+    """The current device, where the kernels run and the tensors must be, and the handle of a stream on it: once a call,
+    as each question costs 0.1 to 0.2 us of a call's 6 to 9."""
+    global _raw_stream_of
+    if _raw_stream_of is None:
+        _load_types()
+        import torch
+        if not torch.cuda.is_available():
+            return None, None                          # (no tensor is on a device then: all are refused)
+        torch.cuda.init()
+        _raw_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: _stream(None))
+    device = _current_device()
+    return device, _raw_stream_of(device) if stream is None else _stream(stream)
+
+
+def _matrix(t, what: str, device=None):
+    """A two-dimensional tensor on the device (None: the current one) with contiguous rows as the bytes of a qsgd_matrix
+    (None for None)."""
     if t is None:
         return None
     kind = (_types or _load_types()).get(t.dtype)
@@ -541,7 +558,8 @@ def _matrix(t, what: str):
     shape = t.shape
     if len(shape) != 2:
         raise ValueError(f"{what} must have two dimensions")
-    _here(t, what)
+    if t.get_device() != device:
+        _here(t, what)
     rows, cols = shape
     ld, step = t.stride()
     if kind == 3:
@@ -577,15 +595,27 @@ def _load_types():
     return _types
 
 
-def _vector(t, n: int, what: str):
-    """Address of a device tensor of n float32 (None for None)."""
+def _vector(t, n: int, what: str, device=None):
+    """Address of a tensor of n float32 on the device (None for None)."""
     if t is None:
         return None
     types = _types or _load_types()
     if types.get(t.dtype) != 0 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous device tensor of {n} float32")
-    _here(t, what)
+    if t.get_device() != device:
+        _here(t, what)
     return t.data_ptr()
+
+
+def _space(t, device=None):
+    """(address, bytes) of a workspace on the device; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.get_device() != device:
+        _here(t, "workspace")
+    if not t.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return t.data_ptr(), t.nbytes
 
 
 def _draws(d):
@@ -594,16 +624,17 @@ def _draws(d):
 
 def qsgd_dropout(draws: Draws, p: float, x, y, residual=None, stream=None) -> None:
     """Queues y = residual + dropout(x); y may be x or residual."""
-    rc = _load().qsgd_dropout(_draws(draws), p, _matrix(x, "x"), _matrix(residual, "residual"),
-                              _matrix(y, "y"), _stream(stream))
+    device, st = _begin(stream)
+    rc = _load().qsgd_dropout(_draws(draws), p, _matrix(x, "x", device), _matrix(residual, "residual", device),
+                              _matrix(y, "y", device), st)
     if rc:
         raise QsgdError(rc, "qsgd_dropout")
 
 
 def qsgd_dropout_backward(draws: Draws, p: float, dy, dx, stream=None) -> None:
     """Queues dx = the gradient of qsgd_dropout's x; dx may be dy."""
-    rc = _load().qsgd_dropout_backward(_draws(draws), p, _matrix(dy, "dy"), _matrix(dx, "dx"),
-                                       _stream(stream))
+    device, st = _begin(stream)
+    rc = _load().qsgd_dropout_backward(_draws(draws), p, _matrix(dy, "dy", device), _matrix(dx, "dx", device), st)
     if rc:
         raise QsgdError(rc, "qsgd_dropout_backward")
 
@@ -616,12 +647,13 @@ def qsgd_quantize(draws, x, rows=None, row_scale=None, columns=None, column_scal
                   rounding: int = ROUND_NEAREST, stream=None) -> None:
     """Queues the levels of x by rows (int8, x's shape) and / or by columns (int8, transposed), and their scales.
     draws: Draws, or None for ROUND_NEAREST."""
-    mx, (n, d) = _matrix(x, "x"), x.shape
-    wp, wbytes = _dev(workspace, "workspace")
+    device, st = _begin(stream)
+    mx, (n, d) = _matrix(x, "x", device), x.shape
+    wp, wbytes = _space(workspace, device)
     rc = _load().qsgd_quantize(_draws(draws), rounding, mx,
-                               _matrix(rows, "rows"), _vector(row_scale, n, "row_scale"),
-                               _matrix(columns, "columns"), _vector(column_scale, d, "column_scale"),
-                               wp, wbytes, _stream(stream))
+                               _matrix(rows, "rows", device), _vector(row_scale, n, "row_scale", device),
+                               _matrix(columns, "columns", device), _vector(column_scale, d, "column_scale", device),
+                               wp, wbytes, st)
     if rc:
         raise QsgdError(rc, "qsgd_quantize")
 
@@ -632,11 +664,12 @@ def qsgd_int_matmul_workspace_bytes(M: int, N: int, K: int) -> int:
 
 def qsgd_int_matmul(a, a_scale, b, b_scale, y, bias=None, workspace=None, stream=None) -> None:
     """Queues y = (a b^T) * a_scale[:, None] * b_scale + bias, a (M x K) and b (N x K) int8."""
-    ma, mb, N = _matrix(a, "a"), _matrix(b, "b"), b.shape[0]
-    wp, wbytes = _dev(workspace, "workspace")
-    rc = _load().qsgd_int_matmul(ma, _vector(a_scale, a.shape[0], "a_scale"), mb,
-                                 _vector(b_scale, N, "b_scale"), _vector(bias, N, "bias"),
-                                 _matrix(y, "y"), wp, wbytes, _stream(stream))
+    device, st = _begin(stream)
+    ma, mb, N = _matrix(a, "a", device), _matrix(b, "b", device), b.shape[0]
+    wp, wbytes = _space(workspace, device)
+    rc = _load().qsgd_int_matmul(ma, _vector(a_scale, a.shape[0], "a_scale", device), mb,
+                                 _vector(b_scale, N, "b_scale", device), _vector(bias, N, "bias", device),
+                                 _matrix(y, "y", device), wp, wbytes, st)
     if rc:
         raise QsgdError(rc, "qsgd_int_matmul")
 
@@ -648,12 +681,12 @@ def qsgd_linear_forward_workspace_bytes(tokens: int, outputs: int, inputs: int) 
 def qsgd_linear_forward(draws, x, w, w_scale, y, bias=None, workspace=None, rounding: int = ROUND_NEAREST,
                         stream=None) -> None:
     """Queues y = Q(x) w^T * w_scale + bias, w (outputs x inputs) int8 as qsgd_quantize left it by rows."""
-    mw, N = _matrix(w, "w"), w.shape[0]
-    wp, wbytes = _dev(workspace, "workspace")
+    device, st = _begin(stream)
+    mw, N = _matrix(w, "w", device), w.shape[0]
+    wp, wbytes = _space(workspace, device)
     rc = _load().qsgd_linear_forward(_draws(draws), rounding,
-                                     _matrix(x, "x"), mw, _vector(w_scale, N, "w_scale"),
-                                     _vector(bias, N, "bias"), _matrix(y, "y"), wp, wbytes,
-                                     _stream(stream))
+                                     _matrix(x, "x", device), mw, _vector(w_scale, N, "w_scale", device),
+                                     _vector(bias, N, "bias", device), _matrix(y, "y", device), wp, wbytes, st)
     if rc:
         raise QsgdError(rc, "qsgd_linear_forward")
 
@@ -665,11 +698,12 @@ def qsgd_linear_backward_workspace_bytes(tokens: int, outputs: int, inputs: int)
 def qsgd_linear_backward(draws, x, w, dy, dx=None, dw=None, db=None, workspace=None,
                          rounding: int = ROUND_NEAREST, stream=None) -> None:
     """Queues the gradients that are asked for: dx (x's type), dw and db (float32)."""
-    mw, N = _matrix(w, "w"), w.shape[0]
-    wp, wbytes = _dev(workspace, "workspace")
+    device, st = _begin(stream)
+    mw, N = _matrix(w, "w", device), w.shape[0]
+    wp, wbytes = _space(workspace, device)
     rc = _load().qsgd_linear_backward(_draws(draws), rounding,
-                                      _matrix(x, "x"), mw, _matrix(dy, "dy"),
-                                      _matrix(dx, "dx"), _matrix(dw, "dw"),
-                                      _vector(db, N, "db"), wp, wbytes, _stream(stream))
+                                      _matrix(x, "x", device), mw, _matrix(dy, "dy", device),
+                                      _matrix(dx, "dx", device), _matrix(dw, "dw", device),
+                                      _vector(db, N, "db", device), wp, wbytes, st)
     if rc:
         raise QsgdError(rc, "qsgd_linear_backward")
