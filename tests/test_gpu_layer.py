@@ -215,6 +215,47 @@ def test_quantize_no_rows_and_no_columns():
     assert bool((got["row_scale"] == 0).all())
 
 
+@pytest.mark.parametrize("rows,cols,dtype,rounding", [(70_001, 1003, torch.float16, 1), (66_000, 1024, torch.bfloat16, 0),
+                                                      (40_000, 1700, torch.float32, 1)], ids=str)
+def test_quantize_columns_of_many_rows(rows, cols, dtype, rounding):
+    """Matrices whose column form takes 512 rows to a workgroup, 128 at a time, and is read past the caches."""
+    x = R.values(rows, cols, dtype, 9)
+    got = quantized(x, rounding, "both")
+    m = x.float().abs().amax(0).cpu().numpy()
+    R.check(got["column_scale"], m.astype(np.float64) / 127, R.U32 * m / 127 * 1.01)
+    inv = np.float32(127) / m
+    some = sorted({0, 1, 127, 128, 511, 512, 640, rows // 2, rows - 100, rows - 2, rows - 1} | set(range(1000, rows, 997)))
+    at = torch.tensor(some, device="cuda")
+    v, levels = R.host(x[at]), got["columns"].t()[at].cpu().numpy().astype(np.int64)
+    for i, r in enumerate(some):
+        t = (v[i] * inv).astype(np.float32).astype(np.float64)
+        if rounding:
+            h = R.half_words(q.Draws(seed=D.seed, stream_id=D.stream_id, iteration=D.iteration, row_base=D.row_base + r), 1, cols)[0]
+            low = np.floor(np.abs(t))
+            want = np.sign(t) * np.minimum(low + ((h + 0.5) / 65536 < np.abs(t) - low), 127)
+        else:
+            want = np.rint(t)
+        assert np.array_equal(levels[i], want), r
+
+
+def test_quantize_past_32_bits_of_elements():
+    """Both forms of a matrix of more than 2^32 elements: its last rows and columns."""
+    rows, cols = 70_016, 65_536
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda").normal_()
+    got = {"rows": torch.empty(rows, cols, dtype=torch.int8, device="cuda"), "row_scale": torch.empty(rows, device="cuda"),
+           "columns": torch.empty(cols, rows, dtype=torch.int8, device="cuda"), "column_scale": torch.empty(cols, device="cuda")}
+    ws = torch.empty(q.qsgd_quantize_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    q.qsgd_quantize(None, x, workspace=ws, rounding=0, **got)
+    for r in (0, 65_535, 65_536, rows - 1):
+        level, scale = R.quantize(x[r:r + 1], 1, 0)
+        assert np.array_equal(got["rows"][r:r + 1].cpu().numpy(), level)
+        R.check(got["row_scale"][r:r + 1], scale, R.U32 * scale * 1.01)
+    for c in (0, 61_345, cols - 1):
+        level, scale = R.quantize(x[:, c:c + 1], 0, 0)
+        assert np.array_equal(got["columns"][c].cpu().numpy(), level[:, 0])
+        R.check(got["column_scale"][c:c + 1], scale, R.U32 * scale * 1.01)
+
+
 def test_quantize_is_unbiased():
     """The mean of 512 stochastic levels times the scale against the value: 2 levels apart at most, so a standard
     deviation of half a level; six of the mean's, plus the half step of a 16-bit draw."""
@@ -382,6 +423,29 @@ def test_product_of_long_sums_and_large_scales(M, N):
         assert bool(((y.double() - want).abs() <= 4 * R.U32 * want).all()), (s, t)
 
 
+def test_product_past_32_bits_of_results():
+    M, N, K = 66_000, 66_001, 48
+    a, b = int_levels(M, K, 1, full=True), int_levels(N, K, 2, full=True)
+    sa, sb = scales(M, 3), scales(N, 4)
+    y = torch.empty(M, N, device="cuda")
+    q.qsgd_int_matmul(a, sa, b, sb, y)
+    at = torch.tensor([0, 1, 65_074, 65_075, M - 1], device="cuda")    # (65075 N is behind 2^32)
+    want, tol = on_device(a[at], sa[at], b, sb)
+    assert bool(((y[at].double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("M", [7, 1100], ids=str)
+def test_product_of_rows_far_apart(M):
+    """Operands that span more than 2^32 bytes, for the kernels of few rows and of tiles."""
+    N, K, ld = 1100, 300, 2 ** 22 + 16
+    a, b = (torch.empty(n, ld, dtype=torch.int8, device="cuda")[:, 1600:1600 + K] for n in (M, N))
+    a.copy_(int_levels(M, K, 1, full=True)), b.copy_(int_levels(N, K, 2, full=True))
+    sa, sb = scales(M, 3), scales(N, 4)
+    y = multiplied(a, sa, b, sb, torch.float32)
+    want, tol = on_device(a, sa, b, sb)
+    assert bool(((y.double() - want).abs() <= tol).all())
+
+
 def test_product_operands_in_larger_matrices():
     """Column ranges of wider matrices: what stands behind K in a row, levels and all, changes nothing."""
     big_a, big_b = int_levels(90, 400, 1, full=True), int_levels(110, 400, 2, full=True)
@@ -495,6 +559,21 @@ def test_linear_backward(M, N, K, dtype):
         got = backward(x, w, dy, rounding)
         for name, (v, tol) in want.items():
             R.check(got[name], v, tol, name)
+
+
+@pytest.mark.parametrize("M,N,K", [(0, 5, 8), (5, 0, 8), (5, 8, 0), (300, 8, 0)], ids=str)
+def test_linear_of_no_tokens_outputs_or_inputs(M, N, K):
+    x, w, ws = torch.ones(M, K, device="cuda"), int_levels(N, K, 1), scales(N, 2)
+    bias = torch.arange(float(N), device="cuda")
+    y = torch.full((M, N), 7.0, device="cuda")
+    work = torch.empty(q.qsgd_linear_forward_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
+    q.qsgd_linear_forward(D, x, w, ws, y, bias=bias, workspace=work, rounding=1)
+    assert torch.equal(y, bias.expand(M, N))
+    dx, dw, db = (torch.full(s, 7.0, device="cuda") for s in ((M, K), (N, K), (N,)))
+    work = torch.empty(q.qsgd_linear_backward_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
+    q.qsgd_linear_backward(D, x, torch.ones(N, K, device="cuda"), torch.ones(M, N, device="cuda"), dx, dw, db, work, 1)
+    # (a NaN or a 7 would say that something was not written)
+    assert bool((dx == 0).all()) and bool((dw == 0).all()) and bool((db == M).all())
 
 
 def test_linear_backward_of_no_tokens():
