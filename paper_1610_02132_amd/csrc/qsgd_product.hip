@@ -181,11 +181,23 @@ __device__ __forceinline__ void leave(const ProductArgs& a, const int16v (&acc)[
   }
 }
 
+// f(0), f(1), ... with numbers that the compiler knows.
+template <uint32_t N, class F>
+__device__ __forceinline__ void static_for(F f) {
+  if constexpr (N > 0) {
+    static_for<N - 1>(f);
+    f(std::integral_constant<uint32_t, N - 1>{});
+  }
+}
+
 template <int MI, int NI, int STAGES>
 __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPair pair) {
   constexpr uint32_t TM = 64 * MI, TN = 64 * NI, kStage = (TM + TN) * kDepth;
   constexpr int kLoads = 2 * (MI + NI);   // of a wavefront and stage, 8 rows each
-  __shared__ __attribute__((aligned(16))) uint8_t s0[kStage], s1[kStage], s2[STAGES > 2 ? kStage : 16], s3[STAGES > 3 ? kStage : 16];
+  __shared__ __attribute__((aligned(16))) uint8_t s0[kStage], s1[kStage];
+  // (each stage an array of its own: the compiler then waits for none but the one that is read)
+  __shared__ __attribute__((aligned(16))) uint8_t s2[STAGES > 2 ? kStage : 16], s3[STAGES > 2 ? kStage : 16];
+  auto place = [&](uint32_t i) -> uint8_t* { return i == 0 ? s0 : i == 1 ? s1 : i == 2 ? s2 : s3; };
   const bool second = blockIdx.x >= pair.first;   // (of two products: the workgroups behind the first one's)
   const ProductArgs& a = pair.of[second];
   uint32_t tm, tn;
@@ -235,83 +247,110 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPai
       for (int j = 0; j < NI; ++j)
         acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[quarter & 1][j], xf[quarter & 1][i], acc[i][j], 0, 0, 0);
   };
-  // Stage `now` has its first quarter in registers when its step begins.  Behind the barrier all wavefronts have read
-  // the stage and hold the next one's loads: its place is loaded again, one part of the loads with the last quarter and
-  // one with the next step's first (`prior` is the stage before), as they come faster than they are taken.
-  constexpr int kPart = kLoads / 2;
-  auto step = [&](uint8_t* now, const uint8_t* next, uint8_t* prior, uint32_t s) {
-    load(s + STAGES - 1, prior, kPart, kLoads, false);
-    read(now, 1);
-    multiply(0);
-    weave<MI * NI, MI + NI, (kLoads - kPart)>();
-    read(now, 2);
-    multiply(1);
-    weave<MI * NI, MI + NI, 0>();
-    read(now, 3);
-    multiply(2);
-    weave<MI * NI, MI + NI, 0>();
-    wait_loads<(STAGES - 2) * kLoads>();
-    meet();
-    load(s + STAGES, now, 0, kPart, false);
-    read(next, 0);
-    multiply(3);
-    weave<MI * NI, MI + NI, kPart>();
-  };
-  auto last_step = [&](uint8_t* now, const uint8_t* next, uint8_t* prior, uint32_t s) {   // ... of the last ones, where loads end
-    if (s + STAGES - 1 < steps) load(s + STAGES - 1, prior, kPart, kLoads, true);
-    read(now, 1);
-    multiply(0);
-    weave<MI * NI, MI + NI, 0>();
-    read(now, 2);
-    multiply(1);
-    weave<MI * NI, MI + NI, 0>();
-    read(now, 3);
-    multiply(2);
-    weave<MI * NI, MI + NI, 0>();
-    if (STAGES > 3 && s + 3 < steps) wait_loads<(STAGES - 2) * kLoads>();
-    else if (STAGES > 2 && s + 2 < steps) wait_loads<kLoads>();
-    else wait_loads<0>();
-    meet();
-    if (s + STAGES < steps) load(s + STAGES, now, 0, kPart, true);
-    read(next, 0);
-    multiply(3);
-  };
-  static_assert(STAGES == 2 || STAGES == 4, "");
-  if (steps > 0) {
-    load(0, s0, 0, kLoads, true);
-    if (steps > 1) load(1, s1, 0, STAGES > 2 ? kLoads : kPart, true);
-    if (STAGES > 2 && steps > 2) load(2, s2, 0, kLoads, true);
-    if (STAGES > 2 && steps > 3) { load(3, s3, 0, kPart, true); wait_loads<(2 * kLoads + kPart)>(); }
-    else if (STAGES > 2 && steps > 2) wait_loads<2 * kLoads>();
-    else if (steps > 1) wait_loads<(STAGES > 2 ? kLoads : kPart)>();
-    else wait_loads<0>();
-    meet();
-    read(s0, 0);
-    uint32_t s = 0;
-    for (; s + 2 * STAGES <= whole; s += STAGES) {
-      if constexpr (STAGES == 2) {
-        step(s0, s1, s1, s);
-        step(s1, s0, s0, s + 1);
-      } else {
-        step(s0, s1, s3, s);
-        step(s1, s2, s0, s + 1);
-        step(s2, s3, s1, s + 2);
-        step(s3, s0, s2, s + 3);
+  if constexpr (STAGES == 2) {
+    // Stage `now` has its first quarter in registers when its step begins.  Behind the barrier all wavefronts have read
+    // the stage and hold the next one's loads: its place is loaded again, one part of the loads with the last quarter and
+    // one with the next step's first, as they come faster than they are taken.
+    constexpr int kPart = kLoads / 2;
+    auto step = [&](uint8_t* now, uint8_t* other, uint32_t s) {
+      load(s + 1, other, kPart, kLoads, false);
+      read(now, 1);
+      multiply(0);
+      weave<MI * NI, MI + NI, (kLoads - kPart)>();
+      read(now, 2);
+      multiply(1);
+      weave<MI * NI, MI + NI, 0>();
+      read(now, 3);
+      multiply(2);
+      weave<MI * NI, MI + NI, 0>();
+      wait_loads<0>();
+      meet();
+      load(s + 2, now, 0, kPart, false);
+      read(other, 0);
+      multiply(3);
+      weave<MI * NI, MI + NI, kPart>();
+    };
+    auto last_step = [&](uint8_t* now, uint8_t* other, uint32_t s) {   // ... of the last ones, where loads end
+      if (s + 1 < steps) load(s + 1, other, kPart, kLoads, true);
+      read(now, 1);
+      multiply(0);
+      weave<MI * NI, MI + NI, 0>();
+      read(now, 2);
+      multiply(1);
+      weave<MI * NI, MI + NI, 0>();
+      read(now, 3);
+      multiply(2);
+      weave<MI * NI, MI + NI, 0>();
+      wait_loads<0>();
+      meet();
+      if (s + 2 < steps) load(s + 2, now, 0, kPart, true);
+      read(other, 0);
+      multiply(3);
+    };
+    if (steps > 0) {
+      load(0, s0, 0, kLoads, true);
+      if (steps > 1) { load(1, s1, 0, kPart, true); wait_loads<kPart>(); }
+      else wait_loads<0>();
+      meet();
+      read(s0, 0);
+      uint32_t s = 0;
+      for (; s + 4 <= whole; s += 2) {
+        step(s0, s1, s);
+        step(s1, s0, s + 1);
+      }
+      for (; s < whole; s += 2) {
+        last_step(s0, s1, s);
+        if (s + 1 < whole) last_step(s1, s0, s + 1);
       }
     }
-    for (; s < whole; s += STAGES) {
-      last_step(s0, s1, STAGES == 2 ? s1 : s3, s);
-      if (s + 1 >= whole) break;
-      last_step(s1, STAGES == 2 ? s0 : s2, s0, s + 1);
-      if (STAGES == 2) continue;
-      if (s + 2 >= whole) break;
-      last_step(s2, s3, s1, s + 2);
-      if (s + 3 >= whole) break;
-      last_step(s3, s0, s2, s + 3);
+  } else {
+    // The next stage is read whole while one is multiplied (333 x 1111 x 2223 8.2 us, a quarter ahead 8.6; eight stages 9.4).
+    // LDS bounds it: 16 KiB written and 32 KiB read are 384 clocks of a stage's 400.
+    static_assert(MI * NI == 1 && STAGES == 4, "");
+    int4v xs[2][4], ws[2][4];
+    auto read_stage = [&](const uint8_t* from, int to) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        ws[to][q] = *reinterpret_cast<const int4v*>(from + (TM + wn) * kDepth + (frag ^ (32 * q)));
+        xs[to][q] = *reinterpret_cast<const int4v*>(from + wm * kDepth + (frag ^ (32 * q)));
+      }
+    };
+    // Waits for all loads but those of the last n stages, n at most MOST.
+    auto wait_stages = [&](auto most, uint32_t n) {
+      static_for<decltype(most)::value + 1>([&](auto i) {
+        if (n == i || (i == decltype(most)::value && n > i)) wait_loads<decltype(i)::value * kLoads>();
+      });
+    };
+    auto step = [&](uint8_t* now, const uint8_t* next, uint32_t s, int held, bool last) {
+      if (!last) wait_loads<(STAGES - 2) * kLoads>();
+      else wait_stages(std::integral_constant<uint32_t, STAGES - 2>{}, s + 2 < steps ? steps - s - 2 : 0);
+      meet();   // all wavefronts have read stage `now` and hold the next one's loads
+      if (!last || s + STAGES < steps) load(s + STAGES, now, 0, kLoads, last);
+      read_stage(next, held ^ 1);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[0][0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(ws[held][q], xs[held][q], acc[0][0], 0, 0, 0);
+      if (!last) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);      // reads of LDS, loads, matrix instructions
+        __builtin_amdgcn_sched_group_barrier(0x20, kLoads, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    if (steps > 0) {
+      static_for<STAGES>([&](auto i) { if (i < steps) load(i, place(i), 0, kLoads, true); });
+      wait_stages(std::integral_constant<uint32_t, STAGES - 1>{}, steps - 1);
+      meet();
+      read_stage(s0, 0);
+      uint32_t s = 0;
+      for (; s + 2 * STAGES <= whole; s += STAGES)
+        static_for<STAGES>([&](auto i) { step(place(i), place((i + 1) % STAGES), s + i, i % 2, false); });
+      for (; s < whole; s += STAGES)
+        static_for<STAGES>([&](auto i) { if (s + i < whole) step(place(i), place((i + 1) % STAGES), s + i, i % 2, true); });
     }
+  }
+  if (steps > 0) {
     if (whole < steps) {   // the part: what lies behind K counts as zero in one of the operands
-      const uint32_t at = whole % STAGES;
-      const uint8_t* now = at == 0 ? s0 : at == 1 ? s1 : at == 2 ? s2 : s3;
+      const uint8_t* now = place(whole % STAGES);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         read(now, q);
@@ -322,6 +361,7 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPai
       }
     }
   }
+  wait_loads<0>();
   meet();   // (all wavefronts have read their last stage)
   // a wavefront's rows of y's tile, written as y's type asks
   uint8_t* stage = (wave < 2 ? s0 : s1) + (wave & 1) * (kStage / 2);
