@@ -305,7 +305,8 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPai
     }
   } else {
     // The next stage is read whole while one is multiplied (333 x 1111 x 2223 8.2 us, a quarter ahead 8.6; eight stages 9.4).
-    // LDS bounds it: 16 KiB written and 32 KiB read are 384 clocks of a stage's 400.
+    // A stage takes 400 clocks: 16 KiB, 41 bytes a clock and compute unit, are what the loads bring; half as many reads of LDS
+    // (every wavefront a quarter of k for the whole tile) take as long.
     static_assert(MI * NI == 1 && STAGES == 4, "");
     int4v xs[2][4], ws[2][4];
     auto read_stage = [&](const uint8_t* from, int to) {
