@@ -55,10 +55,10 @@ __device__ __forceinline__ int4v operand(const int8_t* p, uint64_t ld, uint32_t 
 // one row of y).  128 bytes of k, whole cache lines, are a stage; STAGES of them are in LDS, loaded straight from memory.
 // Slot s of a row of 128 bytes holds chunk s ^ swizzle(row).
 // 8192^3, tiles of 256: 440 us = 2500 Tops, the matrix units busy in 73% of the cycles at a clock that the power of these
-// products brings down to 1.5 to 1.7 GHz (matrix instructions alone on such values: 3040 Tops).  A tile of 256 reads half as many bytes of LDS for a matrix
-// instruction as one of 128 (4096^3 62 us, 128-tiles 69), which a batch of a few thousand results does not fill the
-// card with; the tiles of 64 are for those, with four stages where a compute unit has no second workgroup to hide
-// the loads of one (256 x 4096 x 4096 10.7 us).
+// products brings down to 1.5 to 1.7 GHz (matrix instructions alone on such values: 3040 Tops).  A tile of 256 reads half as
+// many bytes of LDS for a matrix instruction as one of 128 (4096^3 62 us, tiles of 128 70), but small products do not
+// fill the card with such tiles; those of 64 are for them, with four stages where a compute unit has no second workgroup to
+// hide the loads of one (256 x 4096 x 4096 10.6 us, two stages 17.2, tiles of 128 23.1).
 constexpr uint32_t kDepth = 128;   // bytes of k in a stage
 
 // Rows whose 16-byte chunks of one number are read together (8 or 16 neighbours, or fours of them whose numbers differ
@@ -305,8 +305,8 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPai
     }
   } else {
     // The next stage is read whole while one is multiplied (333 x 1111 x 2223 8.2 us, a quarter ahead 8.6; eight stages 9.4).
-    // A stage takes 400 clocks: 16 KiB, 41 bytes a clock and compute unit, are what the loads bring; half as many reads of LDS
-    // (every wavefront a quarter of k for the whole tile) take as long.
+    // A stage takes 400 clocks for 16 load instructions of 1 KiB; half as many reads of LDS (every wavefront a quarter of k for the
+    // whole tile) or loads that read nothing for rows behind the matrix do not shorten it.
     static_assert(MI * NI == 1 && STAGES == 4, "");
     int4v xs[2][4], ws[2][4];
     auto read_stage = [&](const uint8_t* from, int to) {
