@@ -188,6 +188,7 @@ enum ProductKind : uint32_t {
   kProductTile64,     // ... and two
   kProductTile128,
   kProductTile256,
+  kProductShallow,    // little depth, straight from memory, one piece
 };
 struct ProductPlan { uint32_t kind, splits, split_k; uint64_t bytes; };
 // One product, or two that are planned alike and in one piece each.

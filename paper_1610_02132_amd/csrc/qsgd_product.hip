@@ -372,6 +372,45 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPai
   else leave<MI, NI, kStage / 2, QSGD_TYPE_F16>(a, acc, stage, m0 + wm, n0 + wn);
 }
 
+// ---- shallow ----------------------------------------------------------------------
+// Little depth and many results: the results' bytes are what it takes.  Every wavefront makes 32 x 64 of them by itself,
+// operands straight from memory (neighbours share them in the caches), so that nothing waits for a stage and 16
+// wavefronts of a compute unit are at different points of theirs.  8192 x 8192 x 64: fp32 50.3 us = 5.3 TB/s, bf16 41.9.
+constexpr uint32_t kShallowRows = 64, kShallowCols = 128;   // of a workgroup
+
+__global__ __launch_bounds__(256) void k_product_shallow(ProductPair pair) {
+  constexpr uint32_t kRoom = 32 * (64 * 4 + 16) + 32 * 4;
+  __shared__ __attribute__((aligned(16))) uint8_t staged[4][kRoom];
+  const bool second = blockIdx.x >= pair.first;
+  const ProductArgs& a = pair.of[second];
+  uint32_t tm, tn;
+  place_tile(blockIdx.x - (second ? pair.first : 0), (a.M + kShallowRows - 1) / kShallowRows, (a.N + kShallowCols - 1) / kShallowCols, tm, tn);
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t m0 = tm * kShallowRows + (wave & 1) * 32, n0 = tn * kShallowCols + (wave >> 1) * 64;
+  const uint32_t row = lane & 31, own = 16 * (lane >> 5);
+  int16v acc[1][2] = {};
+  for (uint32_t k = 0; k < a.K; k += 128) {
+    int4v x[4], w[4][2];
+#pragma unroll
+    for (uint32_t q = 0; q < 4; ++q) {
+      if (k + 32 * q >= a.K) continue;
+      x[q] = operand(a.a, a.a_ld, m0 + row, a.M, k + 32 * q + own, a.K);
+      w[q][0] = operand(a.b, a.b_ld, n0 + row, a.N, k + 32 * q + own, a.K);
+      w[q][1] = operand(a.b, a.b_ld, n0 + 32 + row, a.N, k + 32 * q + own, a.K);
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < 4; ++q) {
+      if (k + 32 * q >= a.K) continue;
+      if (k + 32 * q + 32 > a.K) x[q] = masked(x[q], k + 32 * q + own, a.K);
+      acc[0][0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[q][0], x[q], acc[0][0], 0, 0, 0);
+      acc[0][1] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[q][1], x[q], acc[0][1], 0, 0, 0);
+    }
+  }
+  if (a.type == QSGD_TYPE_F32) leave<1, 2, kRoom, QSGD_TYPE_F32>(a, acc, staged[wave], m0, n0);
+  else if (a.type == QSGD_TYPE_BF16) leave<1, 2, kRoom, QSGD_TYPE_BF16>(a, acc, staged[wave], m0, n0);
+  else leave<1, 2, kRoom, QSGD_TYPE_F16>(a, acc, staged[wave], m0, n0);
+}
+
 // ---- few rows ---------------------------------------------------------------------
 // At most 32 rows of a: the weights' bytes are what it takes.  A workgroup has 16 of their rows and up to eight wavefronts,
 // which take turns at 256 bytes of k, loaded whole into a wavefront's own piece of LDS and read from there as the matrix
@@ -560,6 +599,12 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
       {kProductTile256, 256, 1, 11.4, 1.3, 1.3},
   };
   constexpr double kLaunch = 2.3, kCus = 256.0;
+  // At most 64 of k (at 128 the loads of 32 bytes from each row cost more than stages) and many results (us, without stages and the
+  // best tiles: 8192 x 8192 x 64 41.9 / 50.2, fp32 50.3 / 59.4; 3968 x 2517 x 34 9.8 / 12.7; 1536 x 1536 x 64 5.4 / 5.7; 1024 x 1024 x 64
+  // 5.2 / 4.5; 8192 x 8192 x 128 68.4 / 49.3), in rows that fill a workgroup's (70000 x 64 x 64 8.1 / 7.8).
+  if (K <= 64 && N >= kShallowCols && (uint64_t)M * N >= 1u << 21 &&
+      (uint64_t)((M + kShallowRows - 1) / kShallowRows) * ((N + kShallowCols - 1) / kShallowCols) < 1u << 23)
+    return {kProductShallow, 1, kMostK, 0};
   const uint32_t fewest = std::max(1u, (K + kMostK - 1) / kMostK);
   auto join = [&](uint32_t splits) { return splits > 1 ? 3.8 + 8.0 * splits * M * N / 7.4e6 : 0.0; };
   ProductPlan best = {};
@@ -592,9 +637,9 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
 
 hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t st) {
   const ProductArgs& a = pair.of[0];
-  auto tiles = [&](auto kernel, uint32_t size) {
+  auto tiles = [&](auto kernel, uint32_t rows, uint32_t cols) {
     ProductPair p = pair;
-    auto count = [&](const ProductArgs& x) { return (x.M + size - 1) / size * ((x.N + size - 1) / size); };
+    auto count = [&](const ProductArgs& x) { return (x.M + rows - 1) / rows * ((x.N + cols - 1) / cols); };
     p.first = count(a);
     const dim3 grid(p.first + (pair.count > 1 ? count(pair.of[1]) : 0), a.splits);
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, p);
@@ -606,10 +651,11 @@ hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t s
     if (a.M <= 16) hipLaunchKernelGGL(k_product_few<1>, grid, block, lds, st, a);
     else hipLaunchKernelGGL(k_product_few<2>, grid, block, lds, st, a);
   }
-  else if (kind == kProductTile64Deep) tiles(k_product<1, 1, 4>, 64);
-  else if (kind == kProductTile64) tiles(k_product<1, 1, 2>, 64);
-  else if (kind == kProductTile128) tiles(k_product<2, 2, 2>, 128);
-  else tiles(k_product<4, 4, 2>, 256);
+  else if (kind == kProductTile64Deep) tiles(k_product<1, 1, 4>, 64, 64);
+  else if (kind == kProductTile64) tiles(k_product<1, 1, 2>, 64, 64);
+  else if (kind == kProductTile128) tiles(k_product<2, 2, 2>, 128, 128);
+  else if (kind == kProductShallow) tiles(k_product_shallow, kShallowRows, kShallowCols);
+  else tiles(k_product<4, 4, 2>, 256, 256);
   return hipGetLastError();
 }
 

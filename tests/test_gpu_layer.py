@@ -341,6 +341,21 @@ def test_product_depths(M, N):
         assert bool(((y.double() - want).abs() <= tol).all()), K
 
 
+@pytest.mark.parametrize("M,N,K", [(1500, 1501, k) for k in (1, 15, 16, 31, 32, 33, 47, 63, 64)] + [(70, 40_000, 17), (16_401, 130, 64), (3, 700_000, 5)],
+                         ids=str)
+def test_product_of_little_depth(M, N, K):
+    a, b = int_levels(M, K, 1, full=True), int_levels(N, K, 2, full=True)
+    sa, sb = scales(M, 3), scales(N, 4)
+    bias = torch.linspace(-2, 2, N, device="cuda")
+    for dtype, with_bias in zip(TYPES, (True, False, True)):
+        y = multiplied(a, sa, b, sb, dtype, bias if with_bias else None, ld=N + 5, start=3)
+        want, tol = on_device(a, sa, b, sb)
+        if with_bias:
+            want, tol = want + bias.double(), tol + R.U32 * (want.abs() + bias.double().abs())
+        tol = tol + R.HALF_STEP[dtype] * want.abs() * 1.01 + R.LEAST[dtype]
+        assert bool(((y.double() - want).abs() <= tol).all()), dtype
+
+
 def test_product_in_pieces():
     """Depths that are summed in pieces and joined, results four to a thread and one."""
     for M, N, K in ((64, 64, 8192), (33, 70, 20_000), (50, 71, 9001), (1500, 1500, 20_000), (300, 302, 16_384)):
@@ -559,6 +574,14 @@ def test_linear_backward(M, N, K, dtype):
         got = backward(x, w, dy, rounding)
         for name, (v, tol) in want.items():
             R.check(got[name], v, tol, name)
+
+
+@pytest.mark.parametrize("M,N,K", [(40, 1500, 1600), (2100, 60, 1100), (60, 64, 40_000), (1, 1460, 1460)], ids=str)
+def test_linear_backward_of_few_tokens_or_outputs(M, N, K):
+    """Gradients of many values and little depth: the weights', the input's, both."""
+    x, w, dy = R.values(M, K, torch.bfloat16, 1), R.values(N, K, torch.bfloat16, 2), R.values(M, N, torch.bfloat16, 3)
+    for name, (v, tol) in expected_gradients(x, w, dy, 1, D).items():
+        R.check(backward(x, w, dy)[name], v, tol, name)
 
 
 @pytest.mark.parametrize("M,N,K", [(0, 5, 8), (5, 0, 8), (5, 8, 0), (300, 8, 0)], ids=str)
