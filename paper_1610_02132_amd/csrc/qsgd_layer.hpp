@@ -160,6 +160,7 @@ struct QuantizeArgs {
   // workgroups (plan_quantize)
   uint32_t row_lanes, row_blocks, max_blocks, tile_blocks;
   bool stream;                // the second launch reads x past the caches
+  bool shared_lines;          // rows do not start at lines of 128 bytes
   uint32_t tile_rows;         // rows that a workgroup of the second launch takes, a multiple of 128
 };
 struct QuantizeJobs { uint32_t count, blocks[2]; QuantizeArgs job[3]; };   // blocks: of the two launches
