@@ -188,6 +188,7 @@ enum ProductKind : uint32_t {
   kProductTile64Deep, // tiles of 64 x 64 results, four stages of k, ...
   kProductTile64,     // ... and two
   kProductTile128,
+  kProductTile128x64,
   kProductTile256,
   kProductShallow,    // little depth, straight from memory, one piece
 };

@@ -58,7 +58,8 @@ __device__ __forceinline__ int4v operand(const int8_t* p, uint64_t ld, uint32_t 
 // products brings down to 1.5 to 1.7 GHz (matrix instructions alone on such values: 3040 Tops).  A tile of 256 reads half as
 // many bytes of LDS for a matrix instruction as one of 128 (4096^3 62 us, tiles of 128 70), but small products do not
 // fill the card with such tiles; those of 64 are for them, with four stages where a compute unit has no second workgroup to
-// hide the loads of one (256 x 4096 x 4096 10.6 us, two stages 17.2, tiles of 128 23.1).
+// hide the loads of one (256 x 4096 x 4096 10.6 us, two stages 17.2, tiles of 128 23.1), and those of 128 x 64 in between
+// (2048^3 14.4 us, tiles of 128 16.4, of 64 17.2).
 constexpr uint32_t kDepth = 128;   // bytes of k in a stage
 
 // Rows whose 16-byte chunks of one number are read together (8 or 16 neighbours, or fours of them whose numbers differ
@@ -587,16 +588,17 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
 // workgroups run in rounds of as many as the 256 compute units hold; a round takes a fixed time and one per stage of
 // 128 bytes of k, longer where several workgroups share a compute unit.  Few rows: the weights' bytes, a's rows that
 // every workgroup reads anew, and the turns of a wavefront.  Fitted to 71 products from 1 x 1024 x 1024 to 8192^3 that
-// every kernel was timed on: the choice takes at most 6% longer than the fastest on 67 of them, 20% on the worst
-// (us, the choice and the fastest: 8 x 500 x 300 5.4 and 4.5, 1500 x 1500 x 4096 23.7 and 20.1, 1024 x 1024 x 32768 52.1 and
-// 47.3, 64 x 1024 x 8192 12.1 and 11.3).
+// every kernel was timed on: the choice takes at most 6% longer than the fastest on 66 of them, 20% on the worst
+// (us, the choice and the fastest: 8 x 500 x 300 5.4 and 4.5, 1500 x 1500 x 4096 22.0 and 20.1, 1024 x 1024 x 32768 51.7 and
+// 47.3, 64 x 1024 x 8192 12.1 and 11.3, 3000 x 1500 x 700 12.3 and 11.6).
 ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
-  struct Kernel { uint32_t kind, size, slots; double fixed, alone, full; };
+  struct Kernel { uint32_t kind, rows, cols, slots; double fixed, alone, full; };
   static constexpr Kernel kernels[] = {
-      {kProductTile64Deep, 64, 2, 2.3, 0.17, 0.37},
-      {kProductTile64, 64, 5, 1.9, 0.24, 1.2},
-      {kProductTile128, 128, 2, 3.2, 0.53, 0.97},
-      {kProductTile256, 256, 1, 11.4, 1.3, 1.3},
+      {kProductTile64Deep, 64, 64, 2, 2.3, 0.17, 0.37},
+      {kProductTile64, 64, 64, 5, 1.9, 0.24, 1.2},
+      {kProductTile128x64, 128, 64, 2, 2.25, 0.39, 0.57},
+      {kProductTile128, 128, 128, 2, 3.2, 0.57, 0.97},
+      {kProductTile256, 256, 256, 1, 11.4, 1.3, 1.3},
   };
   constexpr double kLaunch = 2.3, kCus = 256.0;
   // At most 64 of k (at 128 the loads of 32 bytes from each row cost more than stages) and many results (us, without stages and the
@@ -616,7 +618,7 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
     best = {kind, splits == 1 ? 1 : (K + piece - 1) / piece, piece, 0};
   };
   for (const Kernel& k : kernels) {
-    const double tiles = (double)((M + k.size - 1) / k.size) * ((N + k.size - 1) / k.size), slots = kCus * k.slots;
+    const double tiles = (double)((M + k.rows - 1) / k.rows) * ((N + k.cols - 1) / k.cols), slots = kCus * k.slots;
     if (tiles >= 1 << 23 && k.kind != kProductTile256) continue;   // (a launch has fewer than 2^32 threads)
     for (uint32_t splits = fewest; splits <= 16 * fewest; splits *= 2) {
       if (splits > fewest && (K / splits < 1024 || tiles * splits > 2 * kCus)) break;
@@ -653,6 +655,7 @@ hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t s
   }
   else if (kind == kProductTile64Deep) tiles(k_product<1, 1, 4>, 64, 64);
   else if (kind == kProductTile64) tiles(k_product<1, 1, 2>, 64, 64);
+  else if (kind == kProductTile128x64) tiles(k_product<2, 1, 2>, 128, 64);
   else if (kind == kProductTile128) tiles(k_product<2, 2, 2>, 128, 128);
   else if (kind == kProductShallow) tiles(k_product_shallow, kShallowRows, kShallowCols);
   else tiles(k_product<4, 4, 2>, 256, 256);

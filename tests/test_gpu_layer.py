@@ -326,7 +326,8 @@ def on_device(a, sa, b, sb):
 DEPTHS = ([(20, 300, 256 * j + r) for j in range(0, 18, 4) for r in (1, 15, 16, 255)] +
           [(200, 300, 128 * j + r) for j in range(0, 20) for r in (0, 1, 100, 127) if 128 * j + r > 0] +
           [(1024, 4096, 128 * j + r) for j in range(4, 10) for r in (0, 127)] + [(1030, 4090, 1000), (2500, 2500, 300), (2500, 2470, 129)] +
-          [(4096, 4096, 128 * j + r) for j in range(11, 15) for r in (0, 1)] + [(4090, 4095, 1500), (5000, 5000, 2001)])
+          [(4096, 4096, 128 * j + r) for j in range(11, 15) for r in (0, 1)] + [(4090, 4095, 1500), (5000, 5000, 2001)] +
+          [(2041, 2040, 128 * j + r) for j in range(3, 17) for r in (0, 1, 127)] + [(1000, 4000, 2001), (1024, 4096, 4096)])
 
 
 @pytest.mark.parametrize("M,N", sorted(set(d[:2] for d in DEPTHS)), ids=str)
