@@ -6,6 +6,7 @@ import ctypes as C
 import os
 import struct
 from dataclasses import dataclass
+from operator import index
 
 CODE_SPARSE, CODE_DENSE, CODE_FIXED = 0, 1, 2
 NORM_L2, NORM_MAX = 0, 1
@@ -77,15 +78,23 @@ class Draws:
     iteration_dev: object = None
 
     def c(self) -> bytes:
-        """The bytes of a struct qsgd_draws."""
-        t = self.iteration_dev
-        if t is None:
-            return _pack_draws(self.seed, self.stream_id, self.iteration, self.row_base, 0, 0)
-        if t.numel() != 1 or t.dtype.itemsize != 4 or t.dtype.is_floating_point:
-            raise ValueError("iteration_dev must be a device tensor of one 32-bit integer")
-        _types or _load_types()
-        _here(t, "iteration_dev")
-        return _pack_draws(self.seed, self.stream_id, self.iteration, self.row_base, 0, t.data_ptr())
+        """The bytes of a struct qsgd_draws.  Key, stream and iteration are taken modulo their words, as in Params; a row_base
+        that is no row number is refused."""
+        t, at = self.iteration_dev, 0
+        if t is not None:
+            if t.numel() != 1 or t.dtype.itemsize != 4 or t.dtype.is_floating_point:
+                raise ValueError("iteration_dev must be a device tensor of one 32-bit integer")
+            _types or _load_types()
+            _here(t, "iteration_dev")
+            at = t.data_ptr()
+        try:
+            return _pack_draws(self.seed, self.stream_id, self.iteration, self.row_base, 0, at)
+        except struct.error:             # a field outside its word
+            row_base = index(self.row_base)
+            if not 0 <= row_base < 1 << 32:
+                raise ValueError("row_base must be at least 0 and below 2^32") from None
+            return _pack_draws(index(self.seed) & (1 << 64) - 1, index(self.stream_id) & 0xFFFFFFFF,
+                               index(self.iteration) & 0xFFFFFFFF, row_base, 0, at)
 
 
 _lib = None
