@@ -275,7 +275,8 @@ typedef struct qsgd_matrix {
  * first) of the Philox-4x32-10 block with counter (c / 8, row_base + r, stream_id, iteration)
  * and key seed.  A slice of rows passes the number of its first row as row_base
  * (row_base + rows <= 2^32).  iteration_dev, a word in device memory or NULL, is added to
- * iteration when the kernels run, so that a captured graph draws anew at each replay. */
+ * iteration when the kernels run, so that a captured graph draws anew at each replay; it must
+ * not lie in an output (refused with QSGD_ERR_INVALID_ARG). */
 typedef struct qsgd_draws {
   uint64_t seed;
   uint32_t stream_id;

@@ -64,6 +64,22 @@ bool overlap(const float* p, uint64_t n, const float* q, uint64_t m) {
   return p && q && meet({a, a + 4 * n}, {b, b + 4 * m});
 }
 
+// Whether the word that is added to the iteration lies in an output, which would be written while it is read.
+bool iteration_in(const qsgd_draws* d, const qsgd_matrix* m) {
+  if (!d || !d->iteration_dev || !m || !m->rows || !m->cols) return false;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(d->iteration_dev);
+  const Span to = span(m);
+  if (!meet({at, at + 4}, to)) return false;
+  const uint64_t size = size_of(m->type), ld = m->ld * size;
+  const uint64_t in_row = at < to.from ? 0 : (at - to.from) % ld;   // (between two rows it is in neither)
+  return in_row < m->cols * size || in_row + 4 > ld;
+}
+bool iteration_in(const qsgd_draws* d, const float* p, uint64_t n) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  const uintptr_t word = d ? reinterpret_cast<uintptr_t>(d->iteration_dev) : 0;
+  return p && word && meet({word, word + 4}, {at, at + 4 * n});
+}
+
 bool floats(const float* p, uint64_t n) { return n == 0 || (p && aligned(p, 4)); }
 
 int draw_args(const qsgd_draws* d, uint64_t rows, DrawArgs& a) {
@@ -84,6 +100,7 @@ int dropout(const qsgd_draws* draws, float p, const qsgd_matrix* x, const qsgd_m
   if (residual && (!shaped(residual, x->rows, x->cols) || residual->type != x->type)) return QSGD_ERR_INVALID_ARG;
   if (overlap(x, y) && !same_place(x, y)) return QSGD_ERR_INVALID_ARG;
   if (residual && overlap(residual, y) && !same_place(residual, y)) return QSGD_ERR_INVALID_ARG;
+  if (iteration_in(draws, y)) return QSGD_ERR_INVALID_ARG;
   DropoutArgs a = {};
   if (int rc = draw_args(draws, x->rows, a.draws)) return rc;
   if (x->rows * ((x->cols + 7) / 8) >= kMostThreads) return QSGD_ERR_UNSUPPORTED;
@@ -269,6 +286,8 @@ int qsgd_quantize(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix*
   if (overlap(rs, x->rows, cs, x->cols)) return QSGD_ERR_INVALID_ARG;
   for (const qsgd_matrix* m : {x, rows, columns})
     if (overlap(rs, x->rows, m) || overlap(cs, x->cols, m)) return QSGD_ERR_INVALID_ARG;
+  if (iteration_in(draws, rows) || iteration_in(draws, columns) || iteration_in(draws, rs, x->rows) || iteration_in(draws, cs, x->cols))
+    return QSGD_ERR_INVALID_ARG;
   DrawArgs d = {};
   if (rounding == QSGD_ROUND_STOCHASTIC || draws)
     if (int rc = draw_args(draws, x->rows, d)) return rc;
@@ -316,7 +335,7 @@ int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_m
                         size_t workspace_bytes, void* hip_stream) {
   if (rounding > QSGD_ROUND_STOCHASTIC || !sound(x, false) || !sound(w, true) || !sound(y, false) || x->cols != w->cols ||
       !shaped(y, x->rows, w->rows) || y->type != x->type || !floats(w_scale_dev, w->rows) || !aligned(bias_dev, 4) ||
-      overlap(x, y) || overlap(w, y) || overlap(w_scale_dev, w->rows, y) || overlap(bias_dev, w->rows, y))
+      overlap(x, y) || overlap(w, y) || overlap(w_scale_dev, w->rows, y) || overlap(bias_dev, w->rows, y) || iteration_in(draws, y))
     return QSGD_ERR_INVALID_ARG;
   if (w->ld >= kMostLd || levels_ld(x->cols) >= kMostLd || too_many(y->rows, y->cols)) return QSGD_ERR_UNSUPPORTED;
   DrawArgs d = {};
@@ -367,6 +386,7 @@ int qsgd_linear_backward(const qsgd_draws* draws, uint32_t rounding, const qsgd_
   if (dx && dw && overlap(dx, dw)) return QSGD_ERR_INVALID_ARG;
   for (const qsgd_matrix* m : {x, w, dy, dx, dw})
     if (overlap(db_dev, w->rows, m)) return QSGD_ERR_INVALID_ARG;
+  if (iteration_in(draws, dx) || iteration_in(draws, dw) || iteration_in(draws, db_dev, w->rows)) return QSGD_ERR_INVALID_ARG;
   const uint64_t M = x->rows, N = w->rows, K = x->cols;
   if (levels_ld(N) >= kMostLd || levels_ld(M) >= kMostLd || too_many(M, K) || too_many(N, K)) return QSGD_ERR_UNSUPPORTED;
   DrawArgs d = {};
