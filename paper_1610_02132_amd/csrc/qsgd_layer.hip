@@ -39,7 +39,7 @@ Span span(const qsgd_matrix* m) {
   if (!m->rows || !m->cols) return {p, p};
   return {p, p + ((m->rows - 1) * m->ld + m->cols) * size_of(m->type)};
 }
-bool meet(const Span& a, const Span& b) { return a.from < b.to && b.from < a.to; }
+bool meet(const Span& a, const Span& b) { return a.from < a.to && b.from < b.to && a.from < b.to && b.from < a.to; }
 // Whether two matrices share an element.  Column ranges of one larger matrix (rows equally far apart) do not where the
 // ranges are apart; other matrices whose extents meet count as overlapping.
 bool overlap(const qsgd_matrix* x, const qsgd_matrix* y) {

@@ -1,5 +1,6 @@
-"""The word that is added to the iteration must not lie in an output: a kernel would read it while another writes it.  On the
-host, before anything is queued; the addresses are made up, and a refused call looks at no memory."""
+"""What lies in an output and what does not.  The word that is added to the iteration must not: a kernel would read it while
+another writes it.  Nothing that has no elements does.  On the host, before anything is queued; the addresses are made up, and a
+refused call looks at no memory."""
 import os
 import struct
 
@@ -76,3 +77,13 @@ def test_a_result_without_elements_holds_nothing(L):
     for rows, cols in ((0, 5), (5, 0), (0, 0)):
         y = mat(Y + 2, rows, cols, BF16)
         assert L.qsgd_dropout(draws(Y), 0.1, mat(X, rows, cols, BF16), None, y, None) == 0
+
+
+def test_an_operand_without_elements_overlaps_nothing(L):
+    """Products of no depth whose operands point into the result.  (Refused for their size alone, which is
+    looked at after the overlap: nothing is queued.)"""
+    M, N = 2 ** 20, 2 ** 18
+    y = mat(X, M, N)
+    far, near = X + 2 ** 44, X + 4096
+    for a, b in ((far, far), (near, far), (far, near), (near, near)):
+        assert L.qsgd_int_matmul(mat(a, M, 0, I8), 2 ** 45, mat(b, N, 0, I8), 2 ** 45 + 2 ** 30, None, y, None, 0, None) == UNSUPPORTED
