@@ -129,6 +129,8 @@ ColumnSpace column_space(uint64_t rows, uint64_t cols) {
   s.bytes = 2 * s.sum_at;
   return s;
 }
+// What is enough for it and for every smaller matrix's: its own bytes go up and down with the columns.
+uint64_t most_column_bytes(uint64_t rows, uint64_t cols) { return 2 * padded(4 * column_numbers(rows, cols)); }
 
 QuantizeArgs job(const qsgd_matrix* x, const DrawArgs& draws) {
   QuantizeArgs q = {};
@@ -210,17 +212,20 @@ ProductPlan product_plan(uint64_t M, uint64_t N, uint64_t K) {
   if (!M || !N || too_many(M, N) || K >= kMostLd) return {};   // (nothing to do, or refused)
   return plan_product((uint32_t)M, (uint32_t)N, (uint32_t)K);
 }
-uint64_t product_bytes(uint64_t M, uint64_t N, uint64_t K) { return product_plan(M, N, K).bytes; }
+// What is enough for it and for every smaller one: a plan's own bytes go up and down, as small products are summed in pieces.
+uint64_t most_product_bytes(uint64_t M, uint64_t N, uint64_t K) {
+  return !M || !N || too_many(M, N) || K >= kMostLd ? 0 : product_space(M, N, K);
+}
 
 bool room(const void* ws, size_t have, uint64_t need) { return need == 0 || (ws && aligned(ws, 16) && have >= need); }
 
 // Why a workspace is refused.
 int no_room(const void* ws, uint64_t need) { return need && (!ws || !aligned(ws, 16)) ? QSGD_ERR_INVALID_ARG : QSGD_ERR_CAPACITY; }
 
-// Workspace of the layer: x's levels and scales, then what the product needs.
+// Workspace of the layer: x's levels and scales, then what the product needs.  bytes: of this call; most: of this and every smaller one.
 struct ForwardSpace {
   ProductPlan plan;
-  uint64_t scale, rest, bytes;
+  uint64_t scale, rest, bytes, most;
 };
 ForwardSpace forward_space(uint64_t M, uint64_t N, uint64_t K) {
   ForwardSpace s = {};
@@ -228,6 +233,7 @@ ForwardSpace forward_space(uint64_t M, uint64_t N, uint64_t K) {
   s.scale = padded(M * levels_ld(K));
   s.rest = s.scale + padded(4 * M);
   s.bytes = s.rest + s.plan.bytes;
+  s.most = s.rest + most_product_bytes(M, N, K);
   return s;
 }
 
@@ -235,7 +241,7 @@ ForwardSpace forward_space(uint64_t M, uint64_t N, uint64_t K) {
 // products need, one after the other.
 struct BackwardSpace {
   uint64_t dy_rows, dy_row_scale, w_cols, w_scale, dy_cols, dy_col_scale, x_cols, x_scale;
-  uint64_t dy_space, w_space, x_space, rest, bytes;
+  uint64_t dy_space, w_space, x_space, rest, bytes, most;
   ProductPlan dx, dw;
 };
 BackwardSpace backward_space(uint64_t M, uint64_t N, uint64_t K) {
@@ -246,6 +252,7 @@ BackwardSpace backward_space(uint64_t M, uint64_t N, uint64_t K) {
   s.w_cols = take(K * levels_ld(N)); s.w_scale = take(4 * K);
   s.dy_cols = take(N * levels_ld(M)); s.dy_col_scale = take(4 * N);
   s.x_cols = take(K * levels_ld(M)); s.x_scale = take(4 * K);
+  const uint64_t operands = at;
   s.dy_space = take(column_space(M, N).bytes);
   s.w_space = take(column_space(N, K).bytes);
   s.x_space = take(column_space(M, K).bytes);
@@ -253,6 +260,8 @@ BackwardSpace backward_space(uint64_t M, uint64_t N, uint64_t K) {
   s.dw = product_plan(N, K, M);
   s.rest = take(std::max(s.dx.bytes, s.dw.bytes));
   s.bytes = at;
+  s.most = operands + most_column_bytes(M, N) + most_column_bytes(N, K) + most_column_bytes(M, K) +
+           padded(std::max(most_product_bytes(M, K, N), most_product_bytes(N, K, M)));
   return s;
 }
 
@@ -270,7 +279,7 @@ int qsgd_dropout_backward(const qsgd_draws* draws, float p, const qsgd_matrix* d
 }
 
 size_t qsgd_quantize_workspace_bytes(uint64_t rows, uint64_t cols) {
-  return in_range(rows, cols, 0) && cols ? column_space(rows, cols).bytes : 0;
+  return in_range(rows, cols, 0) && cols ? most_column_bytes(rows, cols) : 0;
 }
 
 int qsgd_quantize(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix* x, const qsgd_matrix* rows,
@@ -291,7 +300,7 @@ int qsgd_quantize(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix*
   DrawArgs d = {};
   if (rounding == QSGD_ROUND_STOCHASTIC || draws)
     if (int rc = draw_args(draws, x->rows, d)) return rc;
-  const uint64_t need = columns ? qsgd_quantize_workspace_bytes(x->rows, x->cols) : 0;
+  const uint64_t need = columns && x->cols ? column_space(x->rows, x->cols).bytes : 0;
   if (!room(workspace_dev, workspace_bytes, need)) return no_room(workspace_dev, need);
   QuantizeJobs jobs = {1, {}, {job(x, d)}};
   if (rows && x->rows) want_rows(jobs.job[0], reinterpret_cast<int8_t*>(rows->data_dev), rows->ld, row_scale_dev);
@@ -302,7 +311,7 @@ int qsgd_quantize(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix*
 }
 
 size_t qsgd_int_matmul_workspace_bytes(uint64_t M, uint64_t N, uint64_t K) {
-  return in_range(M, N, K) ? product_bytes(M, N, K) : 0;
+  return in_range(M, N, K) ? most_product_bytes(M, N, K) : 0;
 }
 
 int qsgd_int_matmul(const qsgd_matrix* a, const float* a_scale_dev, const qsgd_matrix* b, const float* b_scale_dev,
@@ -327,7 +336,7 @@ int qsgd_int_matmul(const qsgd_matrix* a, const float* a_scale_dev, const qsgd_m
 }
 
 size_t qsgd_linear_forward_workspace_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs) {
-  return in_range(tokens, outputs, inputs) ? forward_space(tokens, outputs, inputs).bytes : 0;
+  return in_range(tokens, outputs, inputs) ? forward_space(tokens, outputs, inputs).most : 0;
 }
 
 int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix* x, const qsgd_matrix* w,
@@ -367,7 +376,7 @@ int qsgd_linear_forward(const qsgd_draws* draws, uint32_t rounding, const qsgd_m
 
 size_t qsgd_linear_backward_workspace_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs) {
   if (!in_range(tokens, outputs, inputs) || tokens >= kMostLd || outputs >= kMostLd) return 0;
-  return backward_space(tokens, outputs, inputs).bytes;
+  return backward_space(tokens, outputs, inputs).most;
 }
 
 int qsgd_linear_backward(const qsgd_draws* draws, uint32_t rounding, const qsgd_matrix* x, const qsgd_matrix* w,

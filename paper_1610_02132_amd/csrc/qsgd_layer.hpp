@@ -166,6 +166,8 @@ struct QuantizeArgs {
 struct QuantizeJobs { uint32_t count, blocks[2]; QuantizeArgs job[3]; };   // blocks: of the two launches
 // Lanes to a row of a strip of columns, rows of a chunk, and how many chunks there are.
 void plan_columns(uint32_t rows, uint32_t cols, uint32_t& strip_lanes, uint32_t& chunks, uint32_t& chunk_rows);
+// As many numbers, chunks times columns, as these sizes or any smaller ones have at most.
+uint64_t column_numbers(uint64_t rows, uint64_t cols);
 // Fills in the workgroups of both launches and says how many the larger one has.
 uint64_t plan_quantize(QuantizeJobs& jobs, uint32_t type);
 // First launch: row forms, and the columns' maxima and sums; second: column forms.
@@ -196,6 +198,8 @@ struct ProductPlan { uint32_t kind, splits, split_k; uint64_t bytes; };
 // One product, or two that are planned alike and in one piece each.
 struct ProductPair { ProductArgs of[2]; uint32_t count, first; };
 ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K);
+// Bytes of workspace that are enough for a product of these sizes and for any of smaller ones.
+uint64_t product_space(uint64_t M, uint64_t N, uint64_t K);
 hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t st);
 // The layer on few tokens, x quantized on the way: product has no a and no a_scale.
 struct LinearArgs {

@@ -584,6 +584,12 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
 
 }  // namespace
 
+// Limits of pieces that are made for speed, beyond the fewest that k needs: the estimate takes none outside them (of 400000 products,
+// none of 4096 of k or less, and none with more sums than 256 tiles of 256 have), so that product_space can say what the pieces of
+// any smaller product take.
+constexpr uint32_t kLeastK = 4096, kLeastPiece = 1024, kMorePieces = 16;
+constexpr uint64_t kMostSums = 1u << 24;
+
 // Which kernel, and in how many pieces of k: the one that is expected to take the least time (us).  A tile kernel's
 // workgroups run in rounds of as many as the 256 compute units hold; a round takes a fixed time and one per stage of
 // 128 bytes of k, longer where several workgroups share a compute unit.  Few rows: the weights' bytes, a's rows that
@@ -620,8 +626,8 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
   for (const Kernel& k : kernels) {
     const double tiles = (double)((M + k.rows - 1) / k.rows) * ((N + k.cols - 1) / k.cols), slots = kCus * k.slots;
     if (tiles >= 1 << 23 && k.kind != kProductTile256) continue;   // (a launch has fewer than 2^32 threads)
-    for (uint32_t splits = fewest; splits <= 16 * fewest; splits *= 2) {
-      if (splits > fewest && (K / splits < 1024 || tiles * splits > 2 * kCus)) break;
+    for (uint32_t splits = fewest; splits <= kMorePieces * fewest; splits *= 2) {
+      if (splits > fewest && (K <= kLeastK || K / splits < kLeastPiece || tiles * splits > 2 * kCus || (double)splits * M * N > kMostSums)) break;
       const double stages = std::ceil(K / 128.0 / splits), groups = tiles * splits;
       auto round = [&](double n) {
         const double share = k.slots == 1 ? 0.0 : std::max(0.0, std::ceil(n / kCus) - 1) / (k.slots - 1);
@@ -635,6 +641,14 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
     offer(kProductFew, fewest, kLaunch + 1.4 + (double)N * K / 1.2e7 + (double)M * K * ((N + 15) / 16) / 1.4e7 + 0.65 * std::ceil(K / 2048.0) + join(fewest));
   if (best.splits > 1) best.bytes = (uint64_t)best.splits * M * N * 4;
   return best;
+}
+
+uint64_t product_space(uint64_t M, uint64_t N, uint64_t K) {
+  const uint64_t fewest = std::max<uint64_t>(1, (K + kMostK - 1) / kMostK), least = fewest > 1 ? fewest * M * N : 0;
+  if (K <= kLeastK) return 0;
+  uint64_t splits = kMorePieces * fewest;
+  while (fewest == 1 && K / splits < kLeastPiece) splits /= 2;
+  return 4 * std::max(least, std::min(splits * M * N, kMostSums));
 }
 
 hipError_t launch_products(const ProductPair& pair, uint32_t kind, hipStream_t st) {

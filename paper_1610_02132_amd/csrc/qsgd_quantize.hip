@@ -5,6 +5,8 @@
 // a compute unit).  8192 x 4096 bf16 to the nearest level by rows: 18.7 us = 5.4 TB/s.  With draws the ten rounds of the generator
 // for eight elements cost as much as their levels, and both launches stay behind the memory: gradients of 8192 tokens, 4096 -> 4096
 // bf16, 56 us for 256 MiB (a vector instruction in half of a SIMD's four clocks) and 46 us for 240 MiB (in all of them).
+#include <algorithm>
+
 #include "qsgd_layer.hpp"
 #include "qsgd_levels.hpp"
 
@@ -318,6 +320,11 @@ void plan_columns(uint32_t rows, uint32_t cols, uint32_t& strip_lanes, uint32_t&
   const uint64_t each = (rows + (want < 64 ? want : 64) - 1) / (want < 64 ? want : 64);
   chunk_rows = (uint32_t)(each < least ? least : each);
   chunks = (rows + chunk_rows - 1) / chunk_rows;
+}
+
+// At most 64 chunks, of 64 rows at least, and from 1024 columns on one for each of 512 / strips, rounded up, strips of 128 columns.
+uint64_t column_numbers(uint64_t rows, uint64_t cols) {
+  return std::min(cols * std::min<uint64_t>((rows + 63) / 64, 64), 512 * 128 + cols);
 }
 
 uint64_t plan_quantize(QuantizeJobs& jobs, uint32_t type) {
