@@ -18,12 +18,15 @@ using int16v = __attribute__((ext_vector_type(16))) int;
 constexpr uint32_t kMostK = 130816;
 constexpr uint32_t kSums = 99;   // "type" of a piece's sums in the workspace
 
-// The sum times the row's scale, times the column's, plus the bias, the last two in one rounding.  A row's scale above
-// kBigScale is taken 2^64 times smaller and the product larger again, so that a result overflows only where it has to (a
-// sum is below 2^37); it is a whole number and the scales are not subnormal, so that nothing vanishes on the way.
+// The sum times the row's scale, times the column's, plus the bias, the last two in one rounding.  Where the row's scale is above
+// kBigScale in size the first product, of a sum below 2^37, could leave fp32 although the result does not: it is taken 2^64 times
+// smaller and the column's scale larger, both exactly (the product is at least 2^26 then, so that a column's scale that leaves
+// fp32 on the way belongs to a result that does; a sum of nothing keeps the column's scale).
 constexpr float kBigScale = 0x1p90f;
 __device__ __forceinline__ float result(float sum, float s, float t, float bias) {
-  return s > kBigScale ? sum * (s * 0x1p-64f) * t * 0x1p64f + bias : __builtin_fmaf(sum * s, t, bias);
+  const bool big = fabsf(s) > kBigScale;
+  const float u = big ? sum * (s * 0x1p-64f) : sum * s;
+  return __builtin_fmaf(u, big && u != 0.0f ? t * 0x1p64f : t, bias);
 }
 
 __device__ __forceinline__ void put(const ProductArgs& a, uint32_t m, uint32_t n, float sum, float row_scale) {
@@ -129,7 +132,7 @@ __device__ __forceinline__ void leave(const ProductArgs& a, const int16v (&acc)[
     }
     for (uint32_t r = lane; r < 32 * MI; r += 64) {
       x_scale[r] = a.a_scale[min(m0 + r, a.M - 1)];
-      big |= x_scale[r] > kBigScale;
+      big |= fabsf(x_scale[r]) > kBigScale;
     }
     big = __any(big);
   }
