@@ -280,7 +280,19 @@ typedef struct qsgd_matrix {
  * and key seed.  A slice of rows passes the number of its first row as row_base
  * (row_base + rows <= 2^32).  iteration_dev, a word in device memory or NULL, is added to
  * iteration when the kernels run, so that a captured graph draws anew at each replay; it must
- * not lie in an output (refused with QSGD_ERR_INVALID_ARG). */
+ * not lie in an output (refused with QSGD_ERR_INVALID_ARG).
+ *
+ * A draw is named by (seed, stream_id, iteration), row and column, and by nothing else: calls with
+ * the same name draw the same half-words, whatever for.  That is what makes qsgd_dropout_backward
+ * find the mask of qsgd_dropout; any two others that are to be independent must differ in one of
+ * the three.  qsgd_linear_backward takes stream_id, stream_id + 1 and stream_id + 2 (modulo 2^32),
+ * the other calls stream_id alone, and the blocks of qsgd_encode (stream_id: the peer) are those
+ * of row 0.  With one name for dropout and for the quantizer of what it leaves, for instance, the
+ * kept elements are those of large draws, which round up too rarely: levels are p / 2 too near to
+ * zero in the mean, and the gradient is biased.
+ * A way that uses no draw twice: a seed for the codec; one for each dropout, with stream_id = peer;
+ * one for each layer, with stream_id = 4 peer for qsgd_linear_backward and 4 peer + 3 for its
+ * stochastic qsgd_linear_forward or qsgd_quantize; and the step as iteration. */
 typedef struct qsgd_draws {
   uint64_t seed;
   uint32_t stream_id;
@@ -353,7 +365,8 @@ int qsgd_linear_forward(const qsgd_draws *draws, uint32_t rounding, const qsgd_m
  *   db = sum over the tokens of dy, in fp32        (or NULL)
  * dy draws with stream_id, w with stream_id + 1 (its rows counted from 0), x with
  * stream_id + 2.  With stochastic rounding the factors are independent, so that E dx = dy w and
- * E dw = dy^T x: unbiased estimates of the gradient, as Algorithm 1 asks of g. */
+ * E dw = dy^T x: unbiased estimates of the gradient, as Algorithm 1 asks of g, where x, w and dy
+ * do not depend on the same draws themselves (see qsgd_draws). */
 size_t qsgd_linear_backward_workspace_bytes(uint64_t tokens, uint64_t outputs, uint64_t inputs);
 int qsgd_linear_backward(const qsgd_draws *draws, uint32_t rounding, const qsgd_matrix *x,
                          const qsgd_matrix *w, const qsgd_matrix *dy, const qsgd_matrix *dx,

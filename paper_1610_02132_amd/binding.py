@@ -70,7 +70,12 @@ _pack_draws = struct.Struct("=QIIIIQ").pack
 
 @dataclass
 class Draws:
-    """Mirror of struct qsgd_draws; iteration_dev: a device tensor of one 32-bit integer, or None."""
+    """Mirror of struct qsgd_draws; iteration_dev: a device tensor of one 32-bit integer, or None.
+
+    (seed, stream_id, iteration) name the draws, whatever they are for: a dropout and its backward pass share a name, everything
+    else that is to be independent differs in one of the three (qsgd_linear_backward takes stream_id, + 1 and + 2; the codec's
+    Params draw under the same names).  For instance a seed for the codec, one for each dropout with stream_id = peer, and one for
+    each layer with stream_id = 4 * peer, and 4 * peer + 3 for its stochastic forward pass."""
     seed: int = 0
     stream_id: int = 0
     iteration: int = 0
@@ -706,7 +711,7 @@ def qsgd_linear_backward_workspace_bytes(tokens: int, outputs: int, inputs: int)
 
 def qsgd_linear_backward(draws, x, w, dy, dx=None, dw=None, db=None, workspace=None,
                          rounding: int = ROUND_NEAREST, stream=None) -> None:
-    """Queues the gradients that are asked for: dx (x's type), dw and db (float32)."""
+    """Queues the gradients that are asked for: dx (x's type), dw and db (float32).  Draws under stream_id, + 1 and + 2."""
     device, st = _begin(stream)
     mw, N = _matrix(w, "w", device), w.shape[0]
     wp, wbytes = _space(workspace, device)
