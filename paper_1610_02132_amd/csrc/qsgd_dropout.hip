@@ -12,10 +12,9 @@ namespace {
 template <uint32_t TYPE, bool RESIDUAL, bool STREAM>
 __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a) {
   const uint32_t c8s = (a.cols + 7) / 8, iteration = draw_iteration(a.draws);
-  const uint64_t units = (uint64_t)a.rows * c8s, u = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  if (u >= units) return;
-  const uint32_t r = units >> 32 ? (uint32_t)(u / c8s) : (uint32_t)u / c8s;
-  const uint32_t c8 = (uint32_t)u - r * c8s, c = 8 * c8, n = a.cols - c;
+  const uint32_t u = blockIdx.x * 256 + threadIdx.x;   // (a call has fewer than 2^32 blocks, which is checked before the launch)
+  if (u >= a.rows * c8s) return;
+  const uint32_t r = u / c8s, c8 = u - r * c8s, c = 8 * c8, n = a.cols - c;
   Eight<TYPE> x, z, y;
   x.template load<STREAM>(element_at<TYPE>(a.x, a.x_ld, r, c), n);
   if (RESIDUAL) z.template load<STREAM>(element_at<TYPE>(a.residual, a.residual_ld, r, c), n);

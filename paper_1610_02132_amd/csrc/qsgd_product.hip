@@ -381,6 +381,7 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPai
 // operands straight from memory (neighbours share them in the caches), so that nothing waits for a stage and 16
 // wavefronts of a compute unit are at different points of theirs.  8192 x 8192 x 64: fp32 50.3 us = 5.3 TB/s, bf16 41.9.
 constexpr uint32_t kShallowRows = 64, kShallowCols = 128;   // of a workgroup
+constexpr uint32_t kShallowDepth = 64;                      // most of k: two matrix instructions
 
 __global__ __launch_bounds__(256) void k_product_shallow(ProductPair pair) {
   constexpr uint32_t kRoom = 32 * (64 * 4 + 16) + 32 * 4;
@@ -393,19 +394,17 @@ __global__ __launch_bounds__(256) void k_product_shallow(ProductPair pair) {
   const uint32_t m0 = tm * kShallowRows + (wave & 1) * 32, n0 = tn * kShallowCols + (wave >> 1) * 64;
   const uint32_t row = lane & 31, own = 16 * (lane >> 5);
   int16v acc[1][2] = {};
-  for (uint32_t k = 0; k < a.K; k += 128) {
-    int4v x[4], w[4][2];
+  if (a.K > 0) {
+    int4v x[2], w[2][2];
 #pragma unroll
-    for (uint32_t q = 0; q < 4; ++q) {
-      if (k + 32 * q >= a.K) continue;
-      x[q] = operand(a.a, a.a_ld, m0 + row, a.M, k + 32 * q + own, a.K);
-      w[q][0] = operand(a.b, a.b_ld, n0 + row, a.N, k + 32 * q + own, a.K);
-      w[q][1] = operand(a.b, a.b_ld, n0 + 32 + row, a.N, k + 32 * q + own, a.K);
+    for (uint32_t q = 0; q < 2; ++q) {
+      x[q] = operand(a.a, a.a_ld, m0 + row, a.M, 32 * q + own, a.K);
+      w[q][0] = operand(a.b, a.b_ld, n0 + row, a.N, 32 * q + own, a.K);
+      w[q][1] = operand(a.b, a.b_ld, n0 + 32 + row, a.N, 32 * q + own, a.K);
     }
 #pragma unroll
-    for (uint32_t q = 0; q < 4; ++q) {
-      if (k + 32 * q >= a.K) continue;
-      if (k + 32 * q + 32 > a.K) x[q] = masked(x[q], k + 32 * q + own, a.K);
+    for (uint32_t q = 0; q < 2; ++q) {
+      if (32 * q + 32 > a.K) x[q] = masked(x[q], 32 * q + own, a.K);
       acc[0][0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[q][0], x[q], acc[0][0], 0, 0, 0);
       acc[0][1] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[q][1], x[q], acc[0][1], 0, 0, 0);
     }
@@ -613,7 +612,7 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
   // At most 64 of k (at 128 the loads of 32 bytes from each row cost more than stages) and many results (us, without stages and the
   // best tiles: 8192 x 8192 x 64 41.9 / 50.2, fp32 50.3 / 59.4; 3968 x 2517 x 34 9.8 / 12.7; 1536 x 1536 x 64 5.4 / 5.7; 1024 x 1024 x 64
   // 5.2 / 4.5; 8192 x 8192 x 128 68.4 / 49.3), in rows that fill a workgroup's (70000 x 64 x 64 8.1 / 7.8).
-  if (K <= 64 && N >= kShallowCols && (uint64_t)M * N >= 1u << 21 &&
+  if (K <= kShallowDepth && N >= kShallowCols && (uint64_t)M * N >= 1u << 21 &&
       (uint64_t)((M + kShallowRows - 1) / kShallowRows) * ((N + kShallowCols - 1) / kShallowCols) < 1u << 23)
     return {kProductShallow, 1, kMostK, 0};
   const uint32_t fewest = std::max(1u, (K + kMostK - 1) / kMostK);

@@ -1,5 +1,6 @@
 """Products in pieces by every kernel, in every type, and both gradients of a layer in one launch or in pieces, by every kernel:
 shapes that the host's estimate sends there (see layer_shapes.py)."""
+import numpy as np
 import pytest
 import torch
 
@@ -45,7 +46,12 @@ def within(got, sums, sa, sb, bias, what):
     t = got.dtype
     tol = tol + R.HALF_STEP[t] * (y.abs() + tol) + R.LEAST[t]
     off = (got.double() - y).abs()
-    assert bool((off <= tol).all()), (what, float((off / tol).max()))
+    # a value from half a step above the type's largest on is infinite, one that may be on either side of that is either
+    info = torch.finfo(t)
+    over = info.max + info.eps / 2 * 2.0 ** int(np.log2(info.max))
+    infinite = got.double() == y.sign() * float("inf")
+    right = torch.where(y.abs() - tol >= over, infinite, (off <= tol) | (infinite & (y.abs() + tol >= over)))
+    assert bool(right.all()), (what, float((off / tol)[~right].max()))
 
 
 @pytest.mark.parametrize("M,N,K", list(S.IN_PIECES), ids=str)
@@ -102,3 +108,20 @@ def test_gradients(M, N, K):
         assert torch.equal(got, y), what
     # M terms in some order of additions
     assert bool(((db.double() - dy.double().sum(0)).abs() <= R.U32 * M * dy.double().abs().sum(0) + 1e-45).all())
+
+
+@pytest.mark.parametrize("dtype", R.TYPES, ids=str)
+@pytest.mark.parametrize("M,N,K", [(1500, 1501, k) for k in (0, 1, 31, 32, 33, 64)] + [(1400, 1500, 0)], ids=str)
+def test_product_of_little_or_no_depth(M, N, K, dtype):
+    """Many results of at most two matrix instructions each; of none, where the bias is all there is."""
+    a, b = levels(M, K, 1), levels(N, K, 2)
+    sa, sb = torch.rand(M, device="cuda") + 0.1, torch.rand(N, device="cuda") + 0.1
+    bias = torch.linspace(-3, 3, N, device="cuda")
+    sums = exact_sums(a, b)
+    for with_bias in (None, bias):
+        buf, y = R.framed(M, N, dtype, ld=N + 3, start=1)
+        q.qsgd_int_matmul(a, sa, b, sb, y, bias=with_bias)
+        within(y, sums, sa, sb, with_bias, dtype)
+        assert R.outside_untouched(buf, y)
+        if K == 0:
+            assert torch.equal(y, (torch.zeros(N, device="cuda") if with_bias is None else bias).to(dtype).expand(M, N))
