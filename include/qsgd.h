@@ -249,7 +249,7 @@ int qsgd_pipeline_step(qsgd_pipeline *pl, const qsgd_params *p, uint64_t chunk_e
  * 2^24 rows of more than 2048 columns of the quantizer and 2^26 of any, 2^30 columns quantized by columns, 2^26 rows of
  * an operand, rows of levels 2^23 bytes apart, 2^38 results of a product).
  *
- * The *_workspace_bytes below are host only and never shrink when a size grows (0 for sizes that no call takes): a
+ * The *_workspace_bytes below are host only and, among sizes that a call takes, never shrink when one grows: a
  * workspace made for the largest batch, or for the largest of several layers in each of the three sizes, serves the smaller
  * ones.  What one call itself needs can be less, and a workspace is refused only below that.
  */

@@ -2,7 +2,7 @@
 //   y = residual + [h >= D] x 65536 / (65536 - D),
 // h the 16-bit draw of the element.  A Philox block serves eight neighbouring columns of a row, so
 // a lane takes eight columns: one 16-byte access per matrix for 16-bit types.  HBM bound: 8192 x 4096 bf16 with a
-// residual 33.4 us = 6.0 TB/s, the rate of a plain copy.  One block to a lane: the wavefronts that wait for their
+// residual 33.1 us = 6.1 TB/s, the rate of a plain copy.  One block to a lane: the wavefronts that wait for their
 // loads are hidden by others (1, 2, 4, 8 blocks: 36.6, 37.7, 40.0, 44.7 us with ordinary loads and stores).
 #include "qsgd_layer.hpp"
 

@@ -57,11 +57,11 @@ __device__ __forceinline__ int4v operand(const int8_t* p, uint64_t ld, uint32_t 
 // registers (MFMA 32x32x32: the weights' rows are the rows, so that a lane holds four neighbouring results of
 // one row of y).  128 bytes of k, whole cache lines, are a stage; STAGES of them are in LDS, loaded straight from memory.
 // Slot s of a row of 128 bytes holds chunk s ^ swizzle(row).
-// 8192^3, tiles of 256: 440 us = 2500 Tops, the matrix units busy in 73% of the cycles at a clock that the power of these
-// products brings down to 1.5 to 1.7 GHz (matrix instructions alone on such values: 3040 Tops).  A tile of 256 reads half as
-// many bytes of LDS for a matrix instruction as one of 128 (4096^3 62 us, tiles of 128 70), but small products do not
-// fill the card with such tiles; those of 64 are for them, with four stages where a compute unit has no second workgroup to
-// hide the loads of one (256 x 4096 x 4096 10.6 us, two stages 17.2, tiles of 128 23.1), and those of 128 x 64 in between
+// 8192^3, tiles of 256: 434 to 457 us by the card = 2400 to 2530 Tops, the matrix units busy in 73% of the cycles at a clock that
+// the power of these products brings down to 1.5 to 1.7 GHz (matrix instructions alone on such values: 3040 Tops).  A tile of 256
+// reads half as many bytes of LDS for a matrix instruction as one of 128 (4096^3 60 to 62 us, tiles of 128 70), but small products
+// do not fill the card with such tiles; those of 64 are for them, with four stages where a compute unit has no second workgroup to
+// hide the loads of one (256 x 4096 x 4096 10.2 us, two stages 17.2, tiles of 128 23.1), and those of 128 x 64 in between
 // (2048^3 14.4 us, tiles of 128 16.4, of 64 17.2).
 constexpr uint32_t kDepth = 128;   // bytes of k in a stage
 
@@ -308,9 +308,9 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPai
       }
     }
   } else {
-    // The next stage is read whole while one is multiplied (333 x 1111 x 2223 8.2 us, a quarter ahead 8.6; eight stages 9.4).
-    // A stage takes 400 clocks for 16 load instructions of 1 KiB; half as many reads of LDS (every wavefront a quarter of k for the
-    // whole tile) or loads that read nothing for rows behind the matrix do not shorten it.
+    // The next stage is read whole while one is multiplied (333 x 1111 x 2223, all on one card: 8.2 us, a quarter ahead 8.6, eight
+    // stages 9.4; on other cards up to 9.2).  A stage takes 400 clocks for 16 load instructions of 1 KiB; half as many reads of LDS
+    // (every wavefront a quarter of k for the whole tile) or loads that read nothing for rows behind the matrix do not shorten it.
     static_assert(MI * NI == 1 && STAGES == 4, "");
     int4v xs[2][4], ws[2][4];
     auto read_stage = [&](const uint8_t* from, int to) {
@@ -379,7 +379,8 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPai
 // ---- shallow ----------------------------------------------------------------------
 // Little depth and many results: the results' bytes are what it takes.  Every wavefront makes 32 x 64 of them by itself,
 // operands straight from memory (neighbours share them in the caches), so that nothing waits for a stage and 16
-// wavefronts of a compute unit are at different points of theirs.  8192 x 8192 x 64: fp32 50.3 us = 5.3 TB/s, bf16 41.9.
+// wavefronts of a compute unit are at different points of theirs.  8192 x 8192 x 64: fp32 51.2 us = 5.3 TB/s, bound by
+// the results' bytes; bf16 41.3 = 3.3, which is not, and whose bound is not known.
 constexpr uint32_t kShallowRows = 64, kShallowCols = 128;   // of a workgroup
 constexpr uint32_t kShallowDepth = 64;                      // most of k: two matrix instructions
 
@@ -586,9 +587,9 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs a) {
 
 }  // namespace
 
-// Limits of pieces that are made for speed, beyond the fewest that k needs: the estimate takes none outside them (of 400000 products,
-// none of 4096 of k or less, and none with more sums than 256 tiles of 256 have), so that product_space can say what the pieces of
-// any smaller product take.
+// Limits of pieces that are made for speed, beyond the fewest that k needs, so that product_space can say what any smaller product
+// takes.  Of 500000 products the rest of the estimate would take two outside them, both of 4096 of k, which are faster in one
+// (416 x 2 x 4096 8.7 us, in four pieces 9.1); 2^24 sums are those of 256 tiles of 256.
 constexpr uint32_t kLeastK = 4096, kLeastPiece = 1024, kMorePieces = 16;
 constexpr uint64_t kMostSums = 1u << 24;
 
@@ -610,7 +611,7 @@ ProductPlan plan_product(uint32_t M, uint32_t N, uint32_t K) {
   };
   constexpr double kLaunch = 2.3, kCus = 256.0;
   // At most 64 of k (at 128 the loads of 32 bytes from each row cost more than stages) and many results (us, without stages and the
-  // best tiles: 8192 x 8192 x 64 41.9 / 50.2, fp32 50.3 / 59.4; 3968 x 2517 x 34 9.8 / 12.7; 1536 x 1536 x 64 5.4 / 5.7; 1024 x 1024 x 64
+  // best tiles: 8192 x 8192 x 64 41.3 / 50.2, fp32 50.3 / 59.4; 3968 x 2517 x 34 9.8 / 12.7; 1536 x 1536 x 64 5.4 / 5.7; 1024 x 1024 x 64
   // 5.2 / 4.5; 8192 x 8192 x 128 68.4 / 49.3), in rows that fill a workgroup's (70000 x 64 x 64 8.1 / 7.8).
   if (K <= kShallowDepth && N >= kShallowCols && (uint64_t)M * N >= 1u << 21 &&
       (uint64_t)((M + kShallowRows - 1) / kShallowRows) * ((N + kShallowCols - 1) / kShallowCols) < 1u << 23)

@@ -1,10 +1,13 @@
 // Quantizer Q_s of Sec. 3.1 (Eq. 2) with s = 127 and max scaling (Sec. 4), a bucket being a row or a
 // column of a matrix, levels as signed bytes.  Two launches for any number of matrices: the first makes the row forms and the
 // columns' largest magnitudes (and sums) over chunks of rows, the second the column forms, transposed through LDS.
-// Memory bound: the row form reads a row once, the column form reads the matrix twice (a column does not fit
-// a compute unit).  8192 x 4096 bf16 to the nearest level by rows: 18.7 us = 5.4 TB/s.  With draws the ten rounds of the generator
-// for eight elements cost as much as their levels, and both launches stay behind the memory: gradients of 8192 tokens, 4096 -> 4096
-// bf16, 56 us for 256 MiB (a vector instruction in half of a SIMD's four clocks) and 46 us for 240 MiB (in all of them).
+// The row form reads a row once, the column form reads the matrix twice: the columns of a tall matrix do not fit a compute unit.
+// (Sixteen columns of some 2000 rows of 16 bits would; such short matrices take the same two launches, and a chain of load, maximum
+// and level in each is their time: both forms of 2047 x 1001 fp16 5.8 and 6.0 us.)  Rows of 8192 x 4096 bf16 to the nearest level
+// are bound by memory: 19 to 21 us by the card, 4.8 to 5.2 TB/s.  With draws they take 24 to 25.5; the ten rounds of the generator for
+// eight elements are as many instructions as their levels, but neither the memory nor the instruction slots are full, and what
+// bounds them is not known.  Gradients of 8192 tokens, 4096 -> 4096 bf16: 57 us for 256 MiB (a vector instruction in half of
+// a SIMD's four clocks) and 46 us for 240 MiB (in 97% of them: bound by the instructions).
 #include <algorithm>
 
 #include "qsgd_layer.hpp"
