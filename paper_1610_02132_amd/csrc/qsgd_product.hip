@@ -380,7 +380,7 @@ __global__ __launch_bounds__(256, MI * NI > 4 ? 1 : 2) void k_product(ProductPai
 // Little depth and many results: the results' bytes are what it takes.  Every wavefront makes 32 x 64 of them by itself,
 // operands straight from memory (neighbours share them in the caches), so that nothing waits for a stage and 16
 // wavefronts of a compute unit are at different points of theirs.  8192 x 8192 x 64: fp32 51.2 us = 5.3 TB/s, bound by
-// the results' bytes; bf16 41.3 = 3.3, which is not, and whose bound is not known.
+// the results' bytes; bf16 41.3 = 3.3, bound by the chain of loads, LDS and stores: 3.6 wavefronts on a SIMD wait 63% of their time.
 constexpr uint32_t kShallowRows = 64, kShallowCols = 128;   // of a workgroup
 constexpr uint32_t kShallowDepth = 64;                      // most of k: two matrix instructions
 

@@ -4,10 +4,10 @@
 // The row form reads a row once, the column form reads the matrix twice: the columns of a tall matrix do not fit a compute unit.
 // (Sixteen columns of some 2000 rows of 16 bits would; such short matrices take the same two launches, and a chain of load, maximum
 // and level in each is their time: both forms of 2047 x 1001 fp16 5.8 and 6.0 us.)  Rows of 8192 x 4096 bf16 to the nearest level
-// are bound by memory: 19 to 21 us by the card, 4.8 to 5.2 TB/s.  With draws they take 24 to 25.5; the ten rounds of the generator for
-// eight elements are as many instructions as their levels, but neither the memory nor the instruction slots are full, and what
-// bounds them is not known.  Gradients of 8192 tokens, 4096 -> 4096 bf16: 57 us for 256 MiB (a vector instruction in half of
-// a SIMD's four clocks) and 46 us for 240 MiB (in 97% of them: bound by the instructions).
+// are bound by memory: 19 to 21 us by the card, 4.8 to 5.2 TB/s.  With draws they take 24 to 25.5: the ten rounds of the generator for
+// eight elements are as many instructions as their levels, and over 80% of the slots for vector instructions are taken.  Gradients of 8192
+// tokens, 4096 -> 4096 bf16: 57 us for 256 MiB in the first launch (half of the slots; 5.7 wavefronts on a SIMD wait 65% of their time)
+// and 46 us for 240 MiB in the second (95% of them or more).
 #include <algorithm>
 
 #include "qsgd_layer.hpp"
